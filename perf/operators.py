@@ -227,7 +227,7 @@ def _encode(x):
     top = g.abs().amax(-1)
     bad, tiny = ~torch.isfinite(top), top < 2.0 ** -120
     m, k = torch.frexp(torch.where(bad | tiny, torch.ones_like(top), top))       # top = m * 2^k, m in [0.5, 1)
-    e = torch.where(m <= 0.875, k - 3, k - 2)
+    e = torch.where((m <= 0.875) | (k == 128), k - 3, k - 2)
     e = torch.where(bad | tiny, torch.zeros_like(e), e)
     a = g.abs() * _power(-e[..., None])
     code = sum(((a >= c) if even else (a > c)).to(torch.uint8)
@@ -510,7 +510,7 @@ def _nearest(x):
     top = g.abs().amax(-1, keepdim=True)
     k = torch.floor(torch.log2(top.clamp(min=2.0 ** -140)))
     k = k + (torch.exp2(k + 1) <= top).double() - (torch.exp2(k) > top).double()
-    unit = torch.exp2(torch.where(top <= 1.75 * torch.exp2(k), k - 2, k - 1))
+    unit = torch.exp2(torch.where((top <= 1.75 * torch.exp2(k)) | (k == 127), k - 2, k - 1))
     grid = torch.tensor(_VALUES, dtype=torch.float64, device=x.device)
     far = (g.abs() / unit)[..., None] - grid
     even_first = far.abs() + torch.tensor([0, 1, 0, 1, 0, 1, 0, 1], dtype=torch.float64, device=x.device) * 1e-9
