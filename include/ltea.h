@@ -321,6 +321,68 @@ int ltea_decode_step_lazy(const ltea_cfg *cfg, const void *q, const void *k, con
                           const ltea_cache *cache, int32_t n_seqs, int32_t *status_or_null, void *workspace,
                           size_t workspace_bytes, void *stream);
 
+/* ---- eviction by accumulated attention weight, kept rows in 4 bits --------------------------------------------
+ * A kept set that needs no trained scorer: an entry's key is the attention weight it has received so far, summed over
+ * the query heads of its KV head.  The cache is ltea_cache with these keys in win_score and ret_score (sinks: +inf in
+ * ret_score), and every rule of eviction is the one above with the key in the logit's place (tau_logit: an entry whose
+ * weight is not above it is dropped; 0 drops none that has any).  n_scored = n_seen after these calls.
+ *
+ * ltea_attention_mass: mass[h][j] = sum over the query heads hq of KV head h and the queries i of j's sequence with
+ * j <= i < j + window and i >= n - last (last <= 0: all queries) of exp(scale * q_i . k_j - lse[hq][i]).
+ * lse: [Hq][total_tokens] fp32, the natural log of query i's softmax normaliser (ltea_train_forward writes it); a query
+ * whose lse is not finite counts nothing.  mass: [Hkv][total_tokens] fp32.  q, k: views as in ltea_prefill.  Of the
+ * config budget, sink and tau_logit are ignored.  Same bits every time. */
+size_t ltea_mass_workspace_bytes(const ltea_cfg *cfg, int32_t n_seqs, int64_t total_tokens, int32_t max_seqlen);
+int ltea_attention_mass(const ltea_cfg *cfg, const void *q, int64_t q_stride_tok, int64_t q_stride_head, const void *k,
+                        int64_t k_stride_tok, int64_t k_stride_head, const int32_t *cu_seqlens, int32_t n_seqs,
+                        int64_t total_tokens, int32_t max_seqlen, const float *lse, int32_t last, float *mass,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* Prefill of such a cache: every query of a prompt sees everything before it (cfg->window does not limit the prompt),
+ * mass is taken over the last `last` queries of each sequence (<= 0: all), and ltea_retain on it with rho = 0 fills the
+ * cache.  Arguments as ltea_prefill; mass_or_null, if given, receives the [Hkv][total_tokens] weights. */
+size_t ltea_prefill_mass_workspace_bytes(const ltea_cfg *cfg, int32_t n_seqs, int64_t total_tokens, int32_t max_seqlen);
+int ltea_prefill_mass(const ltea_cfg *cfg, const void *q, int64_t q_stride_tok, int64_t q_stride_head, const void *k,
+                      const void *v, int64_t kv_stride_tok, int64_t kv_stride_head, const int32_t *cu_seqlens,
+                      int32_t n_seqs, int64_t total_tokens, int32_t max_seqlen, int32_t last, void *out,
+                      const ltea_cache *cache, float *mass_or_null, void *workspace, size_t workspace_bytes,
+                      void *stream);
+
+/* Kept rows in 4 bits.  `packed` (device, ltea_packed_bytes bytes, 16-byte aligned) holds the K and V rows of the compact
+ * segments in the place of k_ret and v_ret: 32 channels of a row share a power of two 2^E and hold one of
+ * +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} (codes 0..7, 8 added for the sign) each.  With the largest magnitude m * 2^k, 1 <= m < 2: E = k - 2
+ * for m <= 1.75 and for k = 127, else k - 1; x / 2^E goes to the nearest value, halfway cases to the even code, beyond 6 to 6.  Groups whose largest
+ * magnitude is below 2^-120 are zeros, groups with an infinity or NaN are NaN.  Values are exact in fp32 and bf16, and packing them
+ * again gives the same bytes.
+ * Layout, per (sequence, KV head): ceil(budget/32) blocks of 32 slots, 34 * D bytes each: K codes (16 D), V codes (16 D), K exponent
+ * bytes E + 127 (D; 255: NaN), V exponent bytes (D).  A code byte holds channels d (low half) and d + 1.  Slot r = 8a + 4j + b:
+ *   D = 128: K codes [j][d/32][a][b][16 bytes]   V codes [j][a][d/8][b][4 bytes]
+ *   D =  64: K codes [d/16][a][b][j][8 bytes]    V codes [a][d/4][j][b][2 bytes]
+ *   K exponents [a][b][d/32][j]    V exponents [a][d/32][j][b]
+ * ltea_kept_pack writes the rows of the first ret_count slots of every head from k_ret, v_ret; ltea_kept_unpack writes k_ret, v_ret
+ * from them (to continue a prefill, say).  Other slots and members are not touched: a packed cache shares win_*, ret_score, ret_pos
+ * and the counters with the cache that it was packed from. */
+size_t ltea_packed_bytes(const ltea_cfg *cfg, int32_t n_seqs);
+int ltea_kept_pack(const ltea_cfg *cfg, const ltea_cache *cache, void *packed, int32_t n_seqs, void *stream);
+int ltea_kept_unpack(const ltea_cfg *cfg, const void *packed, const ltea_cache *cache, int32_t n_seqs, void *stream);
+
+/* One decode step that evicts by accumulated weight: steps 2 to 4 of ltea_decode_step with the keys above, after which
+ * the key of every ring and compact entry grows by the weight that q_t's softmax gives it (the incoming token starts
+ * at zero; a weight that is not a number counts nothing), and n_scored = n_seen.  packed_or_null: the compact rows are
+ * there (k_ret, v_ret may then be NULL); the evicted token is attended as it is kept.  At most 128 query heads per KV
+ * head, LTEA_EUNSUPPORTED beyond.  Concurrent calls on the same cache or the same workspace race. */
+size_t ltea_decode_kept_workspace_bytes(const ltea_cfg *cfg, int32_t n_seqs);
+int ltea_decode_step_mass(const ltea_cfg *cfg, const void *q, const void *k, const void *v, void *out,
+                          const ltea_cache *cache, void *packed_or_null, int32_t n_seqs, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+/* ltea_decode_step_lazy over a compact segment in 4 bits: keys are the scores that ltea_rescore writes, n_scored is
+ * left alone, and a token that leaves the window without a final score is reported as there.  Workspace:
+ * ltea_decode_kept_workspace_bytes. */
+int ltea_decode_step_packed(const ltea_cfg *cfg, const void *q, const void *k, const void *v, void *out,
+                            const ltea_cache *cache, void *packed, int32_t n_seqs, int32_t *status_or_null,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- training side (Section 3.1.2 "Adaptive training"; Algorithm 1) -----------------------------------------
  * During training no cap applies: query i sees its window plus every candidate (sink, or logit > tau_logit) that
  * has left it; cfg->budget is ignored by these entry points.  The forward is ltea_prefill's pipeline with the cap

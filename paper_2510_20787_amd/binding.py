@@ -64,7 +64,9 @@ EXPORTS = ["ltea_strerror", "ltea_cnn_panels_bytes", "ltea_cnn_prepare", "ltea_w
            "ltea_append_workspace_bytes",
            "ltea_prefill_append", "ltea_prefill_append_feat", "ltea_decode_feat_workspace_bytes",
            "ltea_decode_step_feat", "ltea_cnn_backward_workspace_bytes", "ltea_cnn_backward", "ltea_lazy_period", "ltea_rescore_workspace_bytes", "ltea_rescore",
-           "ltea_decode_step_lazy", "ltea_train_workspace_bytes", "ltea_train_forward", "ltea_train_backward",
+           "ltea_decode_step_lazy", "ltea_mass_workspace_bytes", "ltea_attention_mass", "ltea_prefill_mass_workspace_bytes",
+           "ltea_prefill_mass", "ltea_packed_bytes", "ltea_kept_pack", "ltea_kept_unpack", "ltea_decode_kept_workspace_bytes",
+           "ltea_decode_step_mass", "ltea_decode_step_packed", "ltea_train_workspace_bytes", "ltea_train_forward", "ltea_train_backward",
            "ltea_lambda_update", "ltea_diag_sink_bytes",
            "ltea_diag_mfma_loop", "ltea_diag_stream_read"]
 
@@ -135,6 +137,27 @@ def lib() -> C.CDLL:
     L.ltea_rescore.argtypes = [P(ltea_cfg), P(ltea_cnn), P(ltea_rope), P(ltea_cache), i32, vp, vp, sz, vp]
     L.ltea_decode_step_lazy.restype = C.c_int
     L.ltea_decode_step_lazy.argtypes = [P(ltea_cfg), vp, vp, vp, vp, P(ltea_cache), i32, vp, vp, sz, vp]
+    L.ltea_mass_workspace_bytes.restype = sz
+    L.ltea_mass_workspace_bytes.argtypes = [P(ltea_cfg), i32, i64, i32]
+    L.ltea_attention_mass.restype = C.c_int
+    L.ltea_attention_mass.argtypes = [P(ltea_cfg), vp, i64, i64, vp, i64, i64, vp, i32, i64, i32, vp, i32, vp, vp, sz, vp]
+    L.ltea_prefill_mass_workspace_bytes.restype = sz
+    L.ltea_prefill_mass_workspace_bytes.argtypes = [P(ltea_cfg), i32, i64, i32]
+    L.ltea_prefill_mass.restype = C.c_int
+    L.ltea_prefill_mass.argtypes = [P(ltea_cfg), vp, i64, i64, vp, vp, i64, i64, vp, i32, i64, i32, i32, vp, P(ltea_cache),
+                                    vp, vp, sz, vp]
+    L.ltea_packed_bytes.restype = sz
+    L.ltea_packed_bytes.argtypes = [P(ltea_cfg), i32]
+    L.ltea_kept_pack.restype = C.c_int
+    L.ltea_kept_pack.argtypes = [P(ltea_cfg), P(ltea_cache), vp, i32, vp]
+    L.ltea_kept_unpack.restype = C.c_int
+    L.ltea_kept_unpack.argtypes = [P(ltea_cfg), vp, P(ltea_cache), i32, vp]
+    L.ltea_decode_kept_workspace_bytes.restype = sz
+    L.ltea_decode_kept_workspace_bytes.argtypes = [P(ltea_cfg), i32]
+    L.ltea_decode_step_mass.restype = C.c_int
+    L.ltea_decode_step_mass.argtypes = [P(ltea_cfg), vp, vp, vp, vp, P(ltea_cache), vp, i32, vp, sz, vp]
+    L.ltea_decode_step_packed.restype = C.c_int
+    L.ltea_decode_step_packed.argtypes = [P(ltea_cfg), vp, vp, vp, vp, P(ltea_cache), vp, i32, vp, vp, sz, vp]
     L.ltea_train_workspace_bytes.restype = sz
     L.ltea_train_workspace_bytes.argtypes = [P(ltea_cfg), P(ltea_cnn), i32, i64, i32]
     L.ltea_train_forward.restype = C.c_int
@@ -488,6 +511,188 @@ def ltea_decode_step_lazy(cfg: ltea_cfg, q: torch.Tensor, k: torch.Tensor, v: to
     _check(lib().ltea_decode_step_lazy(C.byref(cfg), _ptr(q), _ptr(k), _ptr(v), _ptr(out), C.byref(cache.struct), B,
                                        _ptr(status), _ptr(workspace), workspace.numel(), _stream()),
            "ltea_decode_step_lazy")
+    return out
+
+
+def _dense(x: torch.Tensor, shape, dtype: torch.dtype, device, what: str) -> None:
+    """A contiguous tensor of exactly this shape and type, on this device."""
+    assert tuple(x.shape) == tuple(shape) and x.dtype == dtype and x.is_contiguous() and x.device == device, \
+        f"{what}: expected a contiguous {tuple(shape)} {dtype} tensor on {device}"
+
+
+def _on_current_device(x: torch.Tensor, what: str) -> None:
+    """Kernels are enqueued on the current device's current stream."""
+    assert x.device.type == "cuda" and x.device.index == torch.cuda.current_device(), \
+        f"{what}: its device ({x.device}) is not the current one"
+
+
+def _views(cfg: ltea_cfg, q: torch.Tensor, cu_seqlens: torch.Tensor, *kv: torch.Tensor) -> int:
+    """Checks of packed [T, H, D] views and their cu_seqlens; returns the number of sequences."""
+    td = torch.float32 if cfg.dtype == LTEA_F32 else torch.bfloat16
+    T = q.shape[0]
+    assert q.dim() == 3 and tuple(q.shape[1:]) == (cfg.Hq, cfg.D) and q.dtype == td, "q: expected [T, Hq, D] of the config's type"
+    for x in kv:
+        assert tuple(x.shape) == (T, cfg.Hkv, cfg.D) and x.dtype == td and x.device == q.device, "k, v: expected [T, Hkv, D] of the config's type"
+    _dense(cu_seqlens, (cu_seqlens.numel(),), torch.int32, q.device, "cu_seqlens")
+    assert cu_seqlens.numel() >= 1, "cu_seqlens: expected n_seqs + 1 entries"
+    _on_current_device(q, "q")
+    return cu_seqlens.numel() - 1
+
+
+def ltea_mass_workspace_bytes(cfg: ltea_cfg, n_seqs: int, total_tokens: int, max_seqlen: int) -> int:
+    return int(lib().ltea_mass_workspace_bytes(C.byref(cfg), n_seqs, total_tokens, max_seqlen))
+
+
+def ltea_attention_mass(cfg: ltea_cfg, q: torch.Tensor, k: torch.Tensor, cu_seqlens: torch.Tensor, max_seqlen: int,
+                        lse: torch.Tensor, last: int = 0, mass: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The attention weight every token has received from the last `last` queries of its sequence (0: all): [Hkv, T] fp32.
+    lse [Hq, T] fp32: the queries' log normalisers, as ltea_train_forward returns them."""
+    T = q.shape[0]
+    n_seqs = _views(cfg, q, cu_seqlens, k)
+    qst, qsh = _tok_head_strides(q)
+    st, sh = _tok_head_strides(k)
+    _dense(lse, (cfg.Hq, T), torch.float32, q.device, "lse")
+    if mass is None:
+        mass = torch.empty((cfg.Hkv, T), dtype=torch.float32, device=q.device)
+    _dense(mass, (cfg.Hkv, T), torch.float32, q.device, "mass")
+    if workspace is None:
+        workspace = _workspace(ltea_mass_workspace_bytes(cfg, n_seqs, T, max_seqlen), q.device)
+    _check(lib().ltea_attention_mass(C.byref(cfg), _ptr(q), qst, qsh, _ptr(k), st, sh, _ptr(cu_seqlens), n_seqs, T, max_seqlen,
+                                     _ptr(lse), int(last), _ptr(mass), _ptr(workspace), workspace.numel(), _stream()),
+           "ltea_attention_mass")
+    return mass
+
+
+def ltea_prefill_mass_workspace_bytes(cfg: ltea_cfg, n_seqs: int, total_tokens: int, max_seqlen: int) -> int:
+    return int(lib().ltea_prefill_mass_workspace_bytes(C.byref(cfg), n_seqs, total_tokens, max_seqlen))
+
+
+def ltea_prefill_mass(cfg: ltea_cfg, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor,
+                      max_seqlen: int, cache: Cache, last: int = 0, out: Optional[torch.Tensor] = None,
+                      mass: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Prefill of a cache that keeps the entries with the largest accumulated attention weight; the prompt attends to all of
+    itself.  mass (optional, [Hkv, T] fp32) receives the weights."""
+    T = q.shape[0]
+    n_seqs = _views(cfg, q, cu_seqlens, k, v)
+    qst, qsh = _tok_head_strides(q)
+    st, sh = _tok_head_strides(k)
+    assert _tok_head_strides(v) == (st, sh)
+    if out is None:
+        out = torch.empty((T, cfg.Hq, cfg.D), dtype=q.dtype, device=q.device)
+    _dense(out, (T, cfg.Hq, cfg.D), q.dtype, q.device, "out")
+    if mass is not None:
+        _dense(mass, (cfg.Hkv, T), torch.float32, q.device, "mass")
+    if workspace is None:
+        workspace = _workspace(ltea_prefill_mass_workspace_bytes(cfg, n_seqs, T, max_seqlen), q.device)
+    _check_cache(cfg, cache, n_seqs, q)
+    _check(lib().ltea_prefill_mass(C.byref(cfg), _ptr(q), qst, qsh, _ptr(k), _ptr(v), st, sh, _ptr(cu_seqlens), n_seqs, T,
+                                   max_seqlen, int(last), _ptr(out), C.byref(cache.struct), _ptr(mass), _ptr(workspace),
+                                   workspace.numel(), _stream()), "ltea_prefill_mass")
+    return out
+
+
+def _check_cache(cfg: ltea_cfg, cache: Cache, n_seqs: int, like: torch.Tensor, kept_rows: bool = True) -> None:
+    """Sizes and types of a cache for at least n_seqs sequences."""
+    td, dev = like.dtype, like.device
+    f32, i32 = torch.float32, torch.int32
+    want = [("k_win", (cfg.window, cfg.D), td), ("v_win", (cfg.window, cfg.D), td), ("win_score", (cfg.window,), f32),
+            ("ret_count", (), i32)]
+    if cfg.budget > 0:
+        want += [("ret_score", (cfg.budget,), f32), ("ret_pos", (cfg.budget,), i32)]
+        if kept_rows:
+            want += [("k_ret", (cfg.budget, cfg.D), td), ("v_ret", (cfg.budget, cfg.D), td)]
+    for name, shape, dt in want:
+        x = getattr(cache, name)
+        assert x.dim() >= 2 and x.shape[0] >= n_seqs, f"cache.{name}: expected at least {n_seqs} sequences"
+        _dense(x, (x.shape[0], cfg.Hkv, *shape), dt, dev, f"cache.{name}")
+    for name in ("n_seen", "n_scored"):
+        x = getattr(cache, name)
+        assert x.numel() >= n_seqs, f"cache.{name}: expected at least {n_seqs} sequences"
+        _dense(x, (x.numel(),), i32, dev, f"cache.{name}")
+
+
+def ltea_packed_bytes(cfg: ltea_cfg, n_seqs: int) -> int:
+    return int(lib().ltea_packed_bytes(C.byref(cfg), n_seqs))
+
+
+def alloc_packed(cfg: ltea_cfg, n_seqs: int, device="cuda") -> torch.Tensor:
+    """Room for the kept rows of n_seqs sequences in 4 bits, zeroed: [n_seqs, Hkv, blocks of 32 slots, 34 D] bytes."""
+    return torch.zeros((n_seqs, cfg.Hkv, (cfg.budget + 31) // 32, 34 * cfg.D), dtype=torch.uint8, device=device)
+
+
+def _check_packed(cfg: ltea_cfg, packed: torch.Tensor, n_seqs: int, device) -> None:
+    assert packed.dtype == torch.uint8 and packed.is_contiguous() and packed.device == device and \
+        packed.numel() >= ltea_packed_bytes(cfg, n_seqs), "packed: expected the bytes that alloc_packed gives"
+
+
+def ltea_kept_pack(cfg: ltea_cfg, cache: Cache, packed: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The kept rows of every sequence of `cache` in 4 bits."""
+    n_seqs, dev = cache.ret_count.shape[0], cache.ret_count.device
+    if packed is None:
+        packed = alloc_packed(cfg, n_seqs, dev)
+    _convert_kept(cfg, packed, cache, n_seqs)
+    _check(lib().ltea_kept_pack(C.byref(cfg), C.byref(cache.struct), _ptr(packed), n_seqs, _stream()), "ltea_kept_pack")
+    return packed
+
+
+def ltea_kept_unpack(cfg: ltea_cfg, packed: torch.Tensor, cache: Cache) -> Cache:
+    """Writes k_ret and v_ret of `cache` from their 4-bit form."""
+    n_seqs = cache.ret_count.shape[0]
+    _convert_kept(cfg, packed, cache, n_seqs)
+    _check(lib().ltea_kept_unpack(C.byref(cfg), _ptr(packed), C.byref(cache.struct), n_seqs, _stream()), "ltea_kept_unpack")
+    return cache
+
+
+def _convert_kept(cfg: ltea_cfg, packed: torch.Tensor, cache: Cache, n_seqs: int) -> None:
+    td, dev = torch.float32 if cfg.dtype == LTEA_F32 else torch.bfloat16, cache.ret_count.device
+    _on_current_device(cache.ret_count, "cache")
+    _check_packed(cfg, packed, n_seqs, dev)
+    _dense(cache.ret_count, (n_seqs, cfg.Hkv), torch.int32, dev, "cache.ret_count")
+    if cfg.budget > 0:
+        for name in ("k_ret", "v_ret"):
+            _dense(getattr(cache, name), (n_seqs, cfg.Hkv, cfg.budget, cfg.D), td, dev, f"cache.{name}")
+
+
+def ltea_decode_kept_workspace_bytes(cfg: ltea_cfg, n_seqs: int) -> int:
+    return int(lib().ltea_decode_kept_workspace_bytes(C.byref(cfg), n_seqs))
+
+
+def _kept_step_tensors(cfg: ltea_cfg, q, k, v, cache, packed, out, workspace):
+    B = q.shape[0]
+    td = torch.float32 if cfg.dtype == LTEA_F32 else torch.bfloat16
+    _on_current_device(q, "q")
+    for x, h, what in ((q, cfg.Hq, "q"), (k, cfg.Hkv, "k"), (v, cfg.Hkv, "v")):
+        _dense(x, (B, h, cfg.D), td, q.device, what)
+    _check_cache(cfg, cache, B, q, packed is None)
+    if packed is not None:
+        _check_packed(cfg, packed, B, q.device)
+    if out is None:
+        out = torch.empty((B, cfg.Hq, cfg.D), dtype=td, device=q.device)
+    _dense(out, (B, cfg.Hq, cfg.D), td, q.device, "out")
+    if workspace is None:
+        workspace = _workspace(ltea_decode_kept_workspace_bytes(cfg, B), q.device)
+    return B, out, workspace
+
+
+def ltea_decode_step_mass(cfg: ltea_cfg, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: Cache,
+                          packed: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                          workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """A decode step that evicts by accumulated attention weight.  packed: the kept rows in 4 bits, in the place of cache.k_ret
+    and cache.v_ret."""
+    B, out, workspace = _kept_step_tensors(cfg, q, k, v, cache, packed, out, workspace)
+    _check(lib().ltea_decode_step_mass(C.byref(cfg), _ptr(q), _ptr(k), _ptr(v), _ptr(out), C.byref(cache.struct), _ptr(packed), B,
+                                       _ptr(workspace), workspace.numel(), _stream()), "ltea_decode_step_mass")
+    return out
+
+
+def ltea_decode_step_packed(cfg: ltea_cfg, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: Cache, packed: torch.Tensor,
+                            out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                            workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """ltea_decode_step_lazy over kept rows in 4 bits."""
+    B, out, workspace = _kept_step_tensors(cfg, q, k, v, cache, packed, out, workspace)
+    _check(lib().ltea_decode_step_packed(C.byref(cfg), _ptr(q), _ptr(k), _ptr(v), _ptr(out), C.byref(cache.struct), _ptr(packed), B,
+                                         _ptr(status), _ptr(workspace), workspace.numel(), _stream()), "ltea_decode_step_packed")
     return out
 
 

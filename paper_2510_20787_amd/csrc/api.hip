@@ -79,6 +79,16 @@ int check_cache(const ltea_cfg* cfg, const ltea_cache* c, bool need_window) {
   return LTEA_OK;
 }
 
+// The cache of a step over kept entries: packed (or null) stands in the place of k_ret, v_ret.
+int check_kept(const ltea_cfg* cfg, const ltea_cache* c, const void* packed) {
+  if (!c) return LTEA_EINVAL;
+  if (!c->ret_count || !c->n_seen || !c->n_scored || !c->k_win || !c->v_win || !c->win_score) return LTEA_EINVAL;
+  if (cfg->budget > 0 && (!c->ret_score || !c->ret_pos || (!packed && (!c->k_ret || !c->v_ret)))) return LTEA_EINVAL;
+  if (!aligned16(c->k_win) || !aligned16(c->v_win) || !aligned16(packed)) return LTEA_EINVAL;
+  if (!packed && (!aligned16(c->k_ret) || !aligned16(c->v_ret))) return LTEA_EINVAL;
+  return LTEA_OK;
+}
+
 bool use_score_mfma(const ltea_cfg& cfg, const ltea_cnn& cnn) { return score_mfma_supported(cfg, cnn); }
 
 size_t score_workspace(const ltea_cfg& cfg, const ltea_cnn& cnn, int64_t total) {
@@ -548,6 +558,139 @@ int ltea_decode_step_lazy(const ltea_cfg* cfg, const void* q, const void* k, con
   if (workspace && !aligned256(workspace)) return LTEA_EINVAL;
   return hip_status(launch_decode_step_lazy(*cfg, q, k, v, out, *cache, n_seqs, status, workspace,
                                             static_cast<hipStream_t>(stream)));
+}
+
+// ---- accumulated attention weight, kept rows in 4 bits ---------------------------------------------------------------
+size_t ltea_mass_workspace_bytes(const ltea_cfg* cfg, int32_t n_seqs, int64_t total_tokens, int32_t max_seqlen) {
+  if (check_cfg(cfg) != LTEA_OK || n_seqs < 0 || total_tokens < 0 || max_seqlen < 0) return 0;
+  return total_tokens == 0 ? 0 : align_up(mass_workspace_most(*cfg, total_tokens, max_seqlen), 256);
+}
+
+int ltea_attention_mass(const ltea_cfg* cfg, const void* q, int64_t q_stride_tok, int64_t q_stride_head, const void* k,
+                        int64_t k_stride_tok, int64_t k_stride_head, const int32_t* cu_seqlens, int32_t n_seqs,
+                        int64_t total_tokens, int32_t max_seqlen, const float* lse, int32_t last, float* mass, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  int st = check_cfg(cfg);
+  if (st == LTEA_OK) st = check_seqs(cu_seqlens, n_seqs, total_tokens, max_seqlen);
+  if (st != LTEA_OK) return st;
+  if (total_tokens == 0) return LTEA_OK;
+  const int esz = elem_size(cfg->dtype);
+  if ((st = check_view(q, q_stride_tok, q_stride_head, cfg->D, esz)) != LTEA_OK) return st;
+  if ((st = check_view(k, k_stride_tok, k_stride_head, cfg->D, esz)) != LTEA_OK) return st;
+  if (!lse || !mass) return LTEA_EINVAL;
+  SeqView sv{cu_seqlens, n_seqs, total_tokens, max_seqlen};
+  if (!mass_supported(*cfg, sv, last)) return LTEA_EUNSUPPORTED;
+  const size_t need = align_up(mass_workspace(*cfg, sv, last), 256);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return LTEA_EWORKSPACE;
+  if (workspace && !aligned256(workspace)) return LTEA_EINVAL;
+  return hip_status(launch_attention_mass(*cfg, q, q_stride_tok, q_stride_head, k, k_stride_tok, k_stride_head, sv, lse, last, mass,
+                                          workspace, static_cast<hipStream_t>(stream)));
+}
+
+size_t ltea_prefill_mass_workspace_bytes(const ltea_cfg* cfg, int32_t n_seqs, int64_t total_tokens, int32_t max_seqlen) {
+  if (check_cfg(cfg) != LTEA_OK || n_seqs < 0 || total_tokens < 0 || max_seqlen < 0) return 0;
+  if (total_tokens == 0) return 0;
+  return align_up((size_t)cfg->Hq * total_tokens * 4, 256) + align_up((size_t)cfg->Hkv * total_tokens * 4, 256) +
+         align_up(mass_workspace_most(*cfg, total_tokens, max_seqlen), 256);
+}
+
+int ltea_prefill_mass(const ltea_cfg* cfg, const void* q, int64_t q_stride_tok, int64_t q_stride_head, const void* k, const void* v,
+                      int64_t kv_stride_tok, int64_t kv_stride_head, const int32_t* cu_seqlens, int32_t n_seqs,
+                      int64_t total_tokens, int32_t max_seqlen, int32_t last, void* out, const ltea_cache* cache,
+                      float* mass_or_null, void* workspace, size_t workspace_bytes, void* stream) {
+  int st = check_cfg(cfg);
+  if (st == LTEA_OK) st = check_seqs(cu_seqlens, n_seqs, total_tokens, max_seqlen);
+  if (st == LTEA_OK) st = check_cache(cfg, cache, true);
+  if (st != LTEA_OK) return st;
+  if (n_seqs == 0) return LTEA_OK;
+  const int esz = elem_size(cfg->dtype);
+  if (total_tokens > 0) {
+    if ((st = check_view(q, q_stride_tok, q_stride_head, cfg->D, esz)) != LTEA_OK) return st;
+    if ((st = check_view(k, kv_stride_tok, kv_stride_head, cfg->D, esz)) != LTEA_OK) return st;
+    if ((st = check_view(v, kv_stride_tok, kv_stride_head, cfg->D, esz)) != LTEA_OK) return st;
+    if (!out || !aligned16(out)) return LTEA_EINVAL;
+  }
+  // every query of the prompt sees everything before it: the window that counts here is the prompt
+  ltea_cfg open = *cfg;
+  open.window = max_seqlen > 1 ? max_seqlen : 1;
+  open.budget = 0;
+  SeqView sv{cu_seqlens, n_seqs, total_tokens, max_seqlen};
+  if (!mass_supported(open, sv, last)) return LTEA_EUNSUPPORTED;
+  const size_t lse_bytes = align_up((size_t)cfg->Hq * total_tokens * 4, 256);
+  const size_t mass_bytes = mass_or_null ? 0 : align_up((size_t)cfg->Hkv * total_tokens * 4, 256);
+  const size_t need = lse_bytes + mass_bytes + (total_tokens > 0 ? align_up(mass_workspace(open, sv, last), 256) : 0);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return LTEA_EWORKSPACE;
+  if (workspace && !aligned256(workspace)) return LTEA_EINVAL;
+  char* ws = static_cast<char*>(workspace);
+  float* lse = reinterpret_cast<float*>(ws);
+  float* mass = mass_or_null ? mass_or_null : reinterpret_cast<float*>(ws + lse_bytes);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (total_tokens > 0) {
+    st = do_attention(open, q, q_stride_tok, q_stride_head, k, v, kv_stride_tok, kv_stride_head, sv, *cache, out, s, lse);
+    if (st != LTEA_OK) return st;
+    st = hip_status(launch_attention_mass(open, q, q_stride_tok, q_stride_head, k, kv_stride_tok, kv_stride_head, sv, lse, last, mass,
+                                          ws + lse_bytes + mass_bytes, s));
+    if (st != LTEA_OK) return st;
+  }
+  return hip_status(launch_retain(*cfg, mass, k, v, kv_stride_tok, kv_stride_head, sv, 0, *cache, s));
+}
+
+size_t ltea_packed_bytes(const ltea_cfg* cfg, int32_t n_seqs) {
+  if (check_cfg(cfg) != LTEA_OK || n_seqs < 0) return 0;
+  return kept_packed_bytes(*cfg, n_seqs);
+}
+
+namespace {
+int convert_kept(const ltea_cfg* cfg, const ltea_cache* cache, void* packed, bool to_packed, int32_t n_seqs, void* stream) {
+  const int st = check_cfg(cfg);
+  if (st != LTEA_OK) return st;
+  if (!cache || n_seqs < 0) return LTEA_EINVAL;
+  if (n_seqs == 0 || cfg->budget == 0) return LTEA_OK;
+  if (!packed || !cache->k_ret || !cache->v_ret || !cache->ret_count) return LTEA_EINVAL;
+  if (!aligned16(packed) || !aligned16(cache->k_ret) || !aligned16(cache->v_ret)) return LTEA_EINVAL;
+  if ((int64_t)n_seqs * cfg->Hkv > INT32_MAX / (((int64_t)cfg->budget + 31) / 32)) return LTEA_EUNSUPPORTED;
+  return hip_status(launch_kept_convert(*cfg, *cache, packed, to_packed, n_seqs, static_cast<hipStream_t>(stream)));
+}
+
+int kept_step(const ltea_cfg* cfg, const void* q, const void* k, const void* v, void* out, const ltea_cache* cache, void* packed,
+              bool mass, int32_t n_seqs, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
+  int st = check_cfg(cfg);
+  if (st == LTEA_OK) st = check_kept(cfg, cache, packed);
+  if (st != LTEA_OK) return st;
+  if (n_seqs < 0) return LTEA_EINVAL;
+  if (n_seqs == 0) return LTEA_OK;
+  if (!q || !k || !v || !out) return LTEA_EINVAL;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return LTEA_EINVAL;
+  if (!kept_step_supported(*cfg, n_seqs)) return LTEA_EUNSUPPORTED;
+  if (!workspace || workspace_bytes < align_up(kept_workspace(*cfg, n_seqs, packed != nullptr), 256)) return LTEA_EWORKSPACE;
+  if (!aligned256(workspace)) return LTEA_EINVAL;
+  return hip_status(launch_kept_step(*cfg, q, k, v, out, *cache, packed, mass, n_seqs, status, workspace,
+                                     static_cast<hipStream_t>(stream)));
+}
+}  // namespace
+
+int ltea_kept_pack(const ltea_cfg* cfg, const ltea_cache* cache, void* packed, int32_t n_seqs, void* stream) {
+  return convert_kept(cfg, cache, packed, true, n_seqs, stream);
+}
+
+int ltea_kept_unpack(const ltea_cfg* cfg, const void* packed, const ltea_cache* cache, int32_t n_seqs, void* stream) {
+  return convert_kept(cfg, cache, const_cast<void*>(packed), false, n_seqs, stream);
+}
+
+size_t ltea_decode_kept_workspace_bytes(const ltea_cfg* cfg, int32_t n_seqs) {
+  if (check_cfg(cfg) != LTEA_OK || n_seqs < 0 || !kept_step_supported(*cfg, n_seqs)) return 0;
+  return align_up(kept_workspace_most(*cfg, n_seqs), 256);
+}
+
+int ltea_decode_step_mass(const ltea_cfg* cfg, const void* q, const void* k, const void* v, void* out, const ltea_cache* cache,
+                          void* packed_or_null, int32_t n_seqs, void* workspace, size_t workspace_bytes, void* stream) {
+  return kept_step(cfg, q, k, v, out, cache, packed_or_null, true, n_seqs, nullptr, workspace, workspace_bytes, stream);
+}
+
+int ltea_decode_step_packed(const ltea_cfg* cfg, const void* q, const void* k, const void* v, void* out, const ltea_cache* cache,
+                            void* packed, int32_t n_seqs, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!packed) return LTEA_EINVAL;
+  return kept_step(cfg, q, k, v, out, cache, packed, false, n_seqs, status, workspace, workspace_bytes, stream);
 }
 
 size_t ltea_train_workspace_bytes(const ltea_cfg* cfg, const ltea_cnn* cnn, int32_t n_seqs, int64_t total_tokens,

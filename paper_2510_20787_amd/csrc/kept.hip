@@ -1,0 +1,180 @@
+// Launchers of the step over kept entries (kept_step.h), and the conversion of kept rows to 4 bits and back.
+#include "fp4_rows.h"
+#include "kept_run.h"
+
+namespace ltea {
+namespace {
+
+// ---- rows <-> 4 bits ------------------------------------------------------------------------------------------------------------
+// One workgroup per block of 32 rows of a head; a thread takes eight channels of a row at a time, four neighbouring threads a group.
+// Bound: HBM (D = 128, bf16: 512 bytes of row against 136).
+constexpr int kPackThreads = 256;
+
+template <typename T> __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
+  } else {
+    const u32x4 a = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(a[i] << 16); x[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u); }
+  }
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    reinterpret_cast<f32x4*>(p)[0] = f32x4{x[0], x[1], x[2], x[3]};
+    reinterpret_cast<f32x4*>(p)[1] = f32x4{x[4], x[5], x[6], x[7]};
+  } else {
+    bf16x8 a;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] = (bf16_t)x[i];
+    *reinterpret_cast<bf16x8*>(p) = a;
+  }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kPackThreads)
+kept_pack_kernel(const T* __restrict__ k_ret, const T* __restrict__ v_ret, const int32_t* __restrict__ ret_count, int budget,
+                 int n_blocks, uint8_t* __restrict__ packed) {
+  const int64_t head = blockIdx.x / n_blocks;
+  const int blk = (int)(blockIdx.x - head * n_blocks);
+  const int left = ret_count[head] - 32 * blk;
+  if (left <= 0) return;
+  uint8_t* out = packed + (head * n_blocks + blk) * (int64_t)PackGeo<D>::kBlock;
+  constexpr int kItems = 2 * 32 * D / 8;
+#pragma unroll
+  for (int i = threadIdx.x; i < kItems; i += kPackThreads) {
+    const int d = 8 * (i % (D / 8)), r = i / (D / 8) % 32;
+    const bool is_v = i >= kItems / 2;
+    if (r >= left) continue;                 // (whole groups of four threads)
+    float x[8];
+    load8((is_v ? v_ret : k_ret) + (head * budget + 32 * blk + r) * D + d, x);
+    uint32_t top = 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t a = __float_as_uint(x[e]) & 0x7FFFFFFFu;
+      top = a > top ? a : top;
+    }
+#pragma unroll
+    for (int off = 1; off <= 2; off <<= 1) {
+      const uint32_t y = (uint32_t)__shfl_xor((int)top, off, kWave);
+      top = y > top ? y : top;
+    }
+    const uint32_t ex = group_exponent(top);
+    uint32_t codes = 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) codes |= value_code(__float_as_uint(x[e]), ex, top) << (4 * e);
+    if (!is_v) {
+      *reinterpret_cast<uint32_t*>(out + k_code_at<D>(r, d)) = codes;
+    } else if constexpr (D == 128) {
+      *reinterpret_cast<uint32_t*>(out + v_code_at<D>(r, d)) = codes;
+    } else {
+      *reinterpret_cast<uint16_t*>(out + v_code_at<D>(r, d)) = (uint16_t)codes;
+      *reinterpret_cast<uint16_t*>(out + v_code_at<D>(r, d + 4)) = (uint16_t)(codes >> 16);
+    }
+    if (d % 32 == 0) out[is_v ? v_exp_at<D>(r, d / 32) : k_exp_at<D>(r, d / 32)] = (uint8_t)ex;
+  }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kPackThreads)
+kept_unpack_kernel(const uint8_t* __restrict__ packed, const int32_t* __restrict__ ret_count, int budget, int n_blocks,
+                   T* __restrict__ k_ret, T* __restrict__ v_ret) {
+  const int64_t head = blockIdx.x / n_blocks;
+  const int blk = (int)(blockIdx.x - head * n_blocks);
+  const int left = ret_count[head] - 32 * blk;
+  if (left <= 0) return;
+  const uint8_t* in = packed + (head * n_blocks + blk) * (int64_t)PackGeo<D>::kBlock;
+  constexpr int kItems = 2 * 32 * D / 8;
+#pragma unroll
+  for (int i = threadIdx.x; i < kItems; i += kPackThreads) {
+    const int d = 8 * (i % (D / 8)), r = i / (D / 8) % 32;
+    const bool is_v = i >= kItems / 2;
+    if (r >= left) continue;
+    uint32_t codes;
+    if (!is_v || D == 128) codes = *reinterpret_cast<const uint32_t*>(in + (is_v ? v_code_at<D>(r, d) : k_code_at<D>(r, d)));
+    else codes = *reinterpret_cast<const uint16_t*>(in + v_code_at<D>(r, d)) | (uint32_t)*reinterpret_cast<const uint16_t*>(in + v_code_at<D>(r, d + 4)) << 16;
+    const float scale = group_scale(in[is_v ? v_exp_at<D>(r, d / 32) : k_exp_at<D>(r, d / 32)]);
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = code_value(codes >> (4 * e), scale);
+    store8((is_v ? v_ret : k_ret) + (head * budget + 32 * blk + r) * D + d, x);
+  }
+}
+
+// Shares of a head's rows (a workgroup of four waves each).
+int64_t shares_by_rows(const ltea_cfg& cfg, bool packed) {
+  const int64_t row = 2 * cfg.D * (cfg.dtype == LTEA_F32 ? 4 : 2), kept = packed ? 2 * (cfg.D / 2 + cfg.D / 32) : row;
+  const int64_t by_bytes = (cfg.window * row + cfg.budget * kept) / (64 * 1024);
+  const int64_t by_blocks = (kept_blocks_of(cfg.window) + kept_blocks_of(cfg.budget)) / 4;
+  const int64_t n = by_bytes < by_blocks ? by_bytes : by_blocks;
+  return n < 1 ? 1 : n > kKeptMaxShares ? kKeptMaxShares : n;
+}
+constexpr int64_t kKeptWorkgroups = 512;
+int kept_shares(const ltea_cfg& cfg, int n_seqs, bool packed) {
+  const int64_t heads = (int64_t)n_seqs * cfg.Hkv, n = shares_by_rows(cfg, packed), fill = kKeptWorkgroups / heads;
+  return (int)(fill < 1 ? 1 : n < fill ? n : fill);
+}
+
+size_t kept_floats(const ltea_cfg& cfg, int64_t heads, int64_t shares) {
+  const KeptLayout L{cfg.Hq / cfg.Hkv, cfg.D, 1, 32 * (kept_blocks_of(cfg.window) + kept_blocks_of(cfg.budget))};
+  auto up = [](size_t x) { return (x + 63) / 64 * 64; };
+  return up(L.plan() * heads) + up(L.share() * shares) + L.scores() * heads;
+}
+
+}  // namespace
+
+size_t kept_packed_bytes(const ltea_cfg& cfg, int n_seqs) {
+  return (size_t)n_seqs * cfg.Hkv * kept_blocks_of(cfg.budget) * 34 * cfg.D;
+}
+
+size_t kept_workspace(const ltea_cfg& cfg, int n_seqs, bool packed) {
+  const int64_t heads = (int64_t)n_seqs * cfg.Hkv;
+  return heads == 0 ? 0 : kept_floats(cfg, heads, heads * kept_shares(cfg, n_seqs, packed)) * sizeof(float);
+}
+size_t kept_workspace_most(const ltea_cfg& cfg, int n_seqs) {
+  const int64_t heads = (int64_t)n_seqs * cfg.Hkv, by_rows = heads * shares_by_rows(cfg, false);
+  const int64_t shared = by_rows < kKeptWorkgroups ? by_rows : kKeptWorkgroups;
+  return heads == 0 ? 0 : kept_floats(cfg, heads, shared > heads ? shared : heads) * sizeof(float);
+}
+
+bool kept_step_supported(const ltea_cfg& cfg, int n_seqs) {
+  if (cfg.Hq / cfg.Hkv > kKeptMaxGroup) return false;
+  if (cfg.window > (1 << 30) || cfg.budget > (1 << 30)) return false;
+  return (int64_t)n_seqs * cfg.Hkv <= ((int64_t)1 << 24);
+}
+
+hipError_t launch_kept_step(const ltea_cfg& cfg, const void* q, const void* k, const void* v, void* out, const ltea_cache& c,
+                            const void* packed, bool mass, int n_seqs, int32_t* status, void* workspace, hipStream_t stream) {
+  const KeptInputs in{q, k, v, out, packed, status, mass};
+  const int n = kept_shares(cfg, n_seqs, packed != nullptr);
+  if (cfg.dtype == LTEA_F32)
+    return cfg.D == 64 ? kept_run_f32_64(cfg, in, c, n_seqs, n, workspace, stream)
+                       : kept_run_f32_128(cfg, in, c, n_seqs, n, workspace, stream);
+  return cfg.D == 64 ? kept_run_bf16_64(cfg, in, c, n_seqs, n, workspace, stream)
+                     : kept_run_bf16_128(cfg, in, c, n_seqs, n, workspace, stream);
+}
+
+hipError_t launch_kept_convert(const ltea_cfg& cfg, const ltea_cache& c, void* packed, bool to_packed, int n_seqs, hipStream_t stream) {
+  const int n_blocks = kept_blocks_of(cfg.budget);
+  const int64_t grid = (int64_t)n_seqs * cfg.Hkv * n_blocks;
+  if (grid == 0) return hipSuccess;
+  auto go = [&](auto tag, auto dim) {
+    using T = decltype(tag);
+    constexpr int D = decltype(dim)::value;
+    if (to_packed)
+      hipLaunchKernelGGL((kept_pack_kernel<T, D>), dim3((unsigned)grid), dim3(kPackThreads), 0, stream, static_cast<const T*>(c.k_ret),
+                         static_cast<const T*>(c.v_ret), c.ret_count, cfg.budget, n_blocks, static_cast<uint8_t*>(packed));
+    else
+      hipLaunchKernelGGL((kept_unpack_kernel<T, D>), dim3((unsigned)grid), dim3(kPackThreads), 0, stream,
+                         static_cast<const uint8_t*>(packed), c.ret_count, cfg.budget, n_blocks, static_cast<T*>(c.k_ret),
+                         static_cast<T*>(c.v_ret));
+    return hipGetLastError();
+  };
+  if (cfg.dtype == LTEA_F32)
+    return cfg.D == 64 ? go(float{}, std::integral_constant<int, 64>{}) : go(float{}, std::integral_constant<int, 128>{});
+  return cfg.D == 64 ? go(bf16_t{}, std::integral_constant<int, 64>{}) : go(bf16_t{}, std::integral_constant<int, 128>{});
+}
+
+}  // namespace ltea

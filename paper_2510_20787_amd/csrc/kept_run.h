@@ -1,0 +1,35 @@
+// What the launchers (kept.hip) and the kernels (kept_step.h, instantiated per storage type and head size in kept_step_*.hip) of
+// the decode step over a cache that evicts by accumulated attention weight, or whose kept rows are in 4 bits, share.
+#pragma once
+#include "decode_run.h"
+
+namespace ltea {
+
+struct KeptInputs { const void *q, *k, *v; void* out; const void* packed; int32_t* status; bool mass; };
+
+constexpr int kKeptMaxShares = 64;       // lanes of a wave
+constexpr int kKeptMaxGroup = 128;       // query heads per KV head
+
+// What the workgroups of a head hand to the finishing launch, in floats of the workspace.
+struct KeptLayout {
+  int G, D, nsplit, slots;
+  // per head: t, count, bits of the leaving token's key, late; scores of the incoming and of the leaving token [2][G]; V row of the
+  // leaving token as it would be kept [D]
+  __host__ __device__ size_t plan() const { return 4 + 2 * (size_t)G + D; }
+  // per share: its lowest entry (key, position, slot, pad), that entry's scores [G], maximum, sum and output [G][D + 2]
+  __host__ __device__ size_t share() const { return 4 + (size_t)G + (size_t)G * (D + 2); }
+  // per head: the scores of all slots [G][slots]
+  __host__ __device__ size_t scores() const { return (size_t)G * slots; }
+};
+
+inline int kept_blocks_of(int rows) { return (rows + 31) / 32; }
+
+#define LTEA_KEPT_RUN(name)                                                                                       \
+  hipError_t name(const ltea_cfg& cfg, const KeptInputs& in, const ltea_cache& c, int n_seqs, int nsplit, void* workspace, \
+                  hipStream_t stream)
+LTEA_KEPT_RUN(kept_run_f32_64);
+LTEA_KEPT_RUN(kept_run_f32_128);
+LTEA_KEPT_RUN(kept_run_bf16_64);
+LTEA_KEPT_RUN(kept_run_bf16_128);
+
+}  // namespace ltea

@@ -157,6 +157,23 @@ hipError_t launch_decode_step_lazy(const ltea_cfg& cfg, const void* q, const voi
                                    const ltea_cache& cache, int n_seqs, int32_t* status, void* workspace,
                                    hipStream_t stream);
 
+// ---- weights of a prompt, the step that evicts by them, kept rows in 4 bits (attention_mass.hip, kept.hip) --------------------
+size_t mass_workspace(const ltea_cfg& cfg, const SeqView& sv, int last);
+size_t mass_workspace_most(const ltea_cfg& cfg, int64_t total, int32_t max_seqlen);      // of any call of up to so many tokens
+bool mass_supported(const ltea_cfg& cfg, const SeqView& sv, int last);
+hipError_t launch_attention_mass(const ltea_cfg& cfg, const void* q, int64_t q_stride_tok, int64_t q_stride_head, const void* k,
+                                 int64_t k_stride_tok, int64_t k_stride_head, const SeqView& sv, const float* lse, int last,
+                                 float* mass, void* workspace, hipStream_t stream);
+size_t kept_packed_bytes(const ltea_cfg& cfg, int n_seqs);
+size_t kept_workspace(const ltea_cfg& cfg, int n_seqs, bool packed);
+size_t kept_workspace_most(const ltea_cfg& cfg, int n_seqs);                            // of any step of up to so many sequences
+bool kept_step_supported(const ltea_cfg& cfg, int n_seqs);
+// packed (or null): the kept rows in 4 bits, in the place of c.k_ret, c.v_ret.  mass: evicts by accumulated weight, else by the
+// keys as they are.
+hipError_t launch_kept_step(const ltea_cfg& cfg, const void* q, const void* k, const void* v, void* out, const ltea_cache& c,
+                            const void* packed, bool mass, int n_seqs, int32_t* status, void* workspace, hipStream_t stream);
+hipError_t launch_kept_convert(const ltea_cfg& cfg, const ltea_cache& c, void* packed, bool to_packed, int n_seqs, hipStream_t stream);
+
 // ---- backward of the scoring CNN (cnn_backward.hip) ---------------------------------------------------------
 size_t cnn_backward_workspace(const ltea_cfg& cfg, const ltea_cnn& cnn, int64_t total_tokens);
 size_t cnn_backward_workspace_most(const ltea_cfg& cfg, const ltea_cnn& cnn, int64_t total_tokens);   // of any total up to it
