@@ -579,7 +579,7 @@ int ltea_attention_mass(const ltea_cfg* cfg, const void* q, int64_t q_stride_tok
   if ((st = check_view(k, k_stride_tok, k_stride_head, cfg->D, esz)) != LTEA_OK) return st;
   if (!lse || !mass) return LTEA_EINVAL;
   SeqView sv{cu_seqlens, n_seqs, total_tokens, max_seqlen};
-  if (!mass_supported(*cfg, sv, last)) return LTEA_EUNSUPPORTED;
+  if (!mass_supported(*cfg, sv, q_stride_tok, last)) return LTEA_EUNSUPPORTED;
   const size_t need = align_up(mass_workspace(*cfg, sv, last), 256);
   if (need > 0 && (!workspace || workspace_bytes < need)) return LTEA_EWORKSPACE;
   if (workspace && !aligned256(workspace)) return LTEA_EINVAL;
@@ -615,7 +615,7 @@ int ltea_prefill_mass(const ltea_cfg* cfg, const void* q, int64_t q_stride_tok, 
   open.window = max_seqlen > 1 ? max_seqlen : 1;
   open.budget = 0;
   SeqView sv{cu_seqlens, n_seqs, total_tokens, max_seqlen};
-  if (!mass_supported(open, sv, last)) return LTEA_EUNSUPPORTED;
+  if (!mass_supported(open, sv, q_stride_tok, last)) return LTEA_EUNSUPPORTED;
   const size_t lse_bytes = align_up((size_t)cfg->Hq * total_tokens * 4, 256);
   const size_t mass_bytes = mass_or_null ? 0 : align_up((size_t)cfg->Hkv * total_tokens * 4, 256);
   const size_t need = lse_bytes + mass_bytes + (total_tokens > 0 ? align_up(mass_workspace(open, sv, last), 256) : 0);

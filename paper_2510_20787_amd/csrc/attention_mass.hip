@@ -18,43 +18,58 @@ namespace ltea {
 namespace {
 
 constexpr int kThreads = 256, kTileRows = 64;
-template <typename T> constexpr int kKeyBlocks = sizeof(T) == 4 ? 1 : 2;      // of 32 keys per wave
-template <typename T> constexpr int kTileKeys = 4 * 32 * kKeyBlocks<T>;
+// Blocks of 32 keys per wave, keys per workgroup
+template <typename T, int D> constexpr int kKeyBlocks = sizeof(T) == 4 ? 1 : 2;
+template <typename T, int D> constexpr int kTileKeys = 4 * 32 * kKeyBlocks<T, D>;
+int64_t tile_keys(const ltea_cfg& cfg) {
+  if (cfg.dtype == LTEA_F32) return kTileKeys<float, 64>;
+  return cfg.D == 64 ? kTileKeys<bf16_t, 64> : kTileKeys<bf16_t, 128>;
+}
 
 struct MassParams {
-  int n_seqs, tiles_upper, Hq, Hkv, window, last, parts, part_rows;
+  int n_seqs, tiles_upper, Hq, Hkv, window, last, parts, part_rows, units;
   int64_t total;
   float scale2;
 };
 
-// Queries of a sequence of n tokens that can see a key of [lo, hi) and count.
-__device__ __forceinline__ void queries_of(const MassParams& P, int n, int lo, int hi, int& q0, int& q1) {
+// Queries of part `part` of a sequence of n tokens that can see a key of [lo, hi) and count.
+__device__ __forceinline__ void queries_of(const MassParams& P, int part, int n, int lo, int hi, int& q0, int& q1) {
   const int first = P.last > 0 && n > P.last ? n - P.last : 0;
-  q0 = lo > first ? lo : first;
-  const int64_t reach = (int64_t)hi - 1 + P.window;
-  q1 = reach < n ? (int)reach : n;
+  const int64_t from = first + (int64_t)part * P.part_rows, reach = (int64_t)hi - 1 + P.window;
+  const int64_t to = from + P.part_rows < reach ? from + P.part_rows : reach;
+  q0 = (int)(from < lo ? lo / kTileRows * kTileRows > from ? lo / kTileRows * kTileRows : from : from < n ? from : n);
+  q1 = (int)(to < n ? to : n);
 }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 2)
 attention_mass_kernel(const T* __restrict__ q, int64_t q_st, int64_t q_sh, const T* __restrict__ k, int64_t k_st, int64_t k_sh,
                       const int32_t* __restrict__ cu, const float* __restrict__ lse, MassParams P, float* __restrict__ sums) {
-  constexpr int KB = kKeyBlocks<T>, kKeys = kTileKeys<T>;
+  constexpr int KB = kKeyBlocks<T, D>, kKeys = kTileKeys<T, D>;
   constexpr int kRow = D * (int)sizeof(T), PPR = kRow / 16, KP = PPR / 2;       // 16-byte pieces of a row, and per lane
   constexpr int kLoads = kTileRows * PPR / kThreads;
   __shared__ __align__(1024) uint8_t tile[2][kTileRows * kRow];
   __shared__ float tile_lse[2][kTileRows];
+  __shared__ int tile_whole[2];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), c = lane & 31, hb = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int part = blockIdx.x % P.parts, h = blockIdx.x / P.parts % P.Hkv, flat = blockIdx.x / P.parts / P.Hkv;
+  // An XCD takes whole (part, KV head) units: the key tiles that read the same queries run side by side on its L2.  Late parts, which
+  // the most keys see, first.
+  const int unit = (int)(blockIdx.x % 8 + blockIdx.x / 8 / P.tiles_upper * 8), flat = (int)(blockIdx.x / 8 % P.tiles_upper);
+  if (unit >= P.units) return;
+  const int part = P.parts - 1 - unit / P.Hkv, h = unit % P.Hkv;
   int seq, tile_i, lo, n;
   if (!locate_tile(cu, P.n_seqs, kKeys, flat, seq, tile_i, lo, n)) return;
   const int key0 = tile_i * kKeys, key1 = key0 + kKeys < n ? key0 + kKeys : n;
   int q0, q1;
-  queries_of(P, n, key0, key1, q0, q1);
-  q0 += part * P.part_rows;
-  q1 = q1 < q0 + P.part_rows ? q1 : q0 + P.part_rows;
+  queries_of(P, part, n, key0, key1, q0, q1);
   const int G = P.Hq / P.Hkv;
+
+  float* to = sums + ((int64_t)part * P.Hkv + h) * P.total + lo;
+  if (q1 <= q0) {
+    for (int j = key0 + tid; j < key1; j += kThreads) to[j] = 0.f;
+    return;
+  }
 
   // this wave's keys
   const int my0 = key0 + wave * 32 * KB;
@@ -72,89 +87,131 @@ attention_mass_kernel(const T* __restrict__ q, int64_t q_st, int64_t q_sh, const
 #pragma unroll
     for (int r = 0; r < 16; ++r) sum[x][r] = 0.f;
 
-  const int per_head = q1 > q0 ? (q1 - q0 + kTileRows - 1) / kTileRows : 0, tiles = per_head * G;
   // piece p of row r lies at p ^ swizzle(r): sixteen consecutive rows at one piece then cover all banks
   auto swizzle = [](int r) { return PPR == 8 ? (r >> 1) & 7 : r & 15; };
+  const uint32_t row_bytes = (uint32_t)(q_st * (int64_t)sizeof(T));
+  uint32_t from[kLoads], into[kLoads];                     // of this thread's pieces: in memory from the tile's first row, in the LDS tile
+#pragma unroll
+  for (int x = 0; x < kLoads; ++x) {
+    const int piece = tid + kThreads * x, r = piece / PPR, p = piece % PPR;
+    from[x] = (uint32_t)r * row_bytes + 16u * p;
+    into[x] = (uint32_t)(r * kRow + 16 * (p ^ swizzle(r)));
+  }
   u32x4 held[kLoads];
   float held_lse = 0.f;
-  auto request = [&](int i) {
-    const int g = i / per_head, r0 = q0 + (i - g * per_head) * kTileRows;
-    const T* base = q + (int64_t)lo * q_st + (int64_t)(h * G + g) * q_sh;
+  // the tile of query head h * G + g from row r0 on: rows past the sequence's end read as zeros
+  auto request = [&](int g, int r0) {
+    const T* base = q + (int64_t)(lo + r0) * q_st + (int64_t)(h * G + g) * q_sh;
+    const int rows = n - r0 < kTileRows ? n - r0 : kTileRows;
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, (uint32_t)(rows - 1) * row_bytes + (uint32_t)kRow, 0x00020000);
 #pragma unroll
-    for (int x = 0; x < kLoads; ++x) {
-      const int piece = tid + kThreads * x, r = piece / PPR;
-      const int row = r0 + r < n ? r0 + r : n - 1;
-      held[x] = reinterpret_cast<const u32x4*>(base + (int64_t)row * q_st)[piece % PPR];
-    }
-    if (tid < kTileRows) {
-      const float y = r0 + tid < q1 ? lse[(int64_t)(h * G + g) * P.total + lo + r0 + tid] : INFINITY;
-      held_lse = fabsf(y) < INFINITY ? y * 1.4426950408889634f : INFINITY;       // no query, or one whose lse is not finite: counts nothing
+    for (int x = 0; x < kLoads; ++x) held[x] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, from[x], 0, 0);
+    if (wave == 0) held_lse = lse[(int64_t)(h * G + g) * P.total + lo + (r0 + lane < n ? r0 + lane : n - 1)];
+  };
+  auto put = [&](int buf, int r0) {
+#pragma unroll
+    for (int x = 0; x < kLoads; ++x) *reinterpret_cast<u32x4*>(&tile[buf][into[x]]) = held[x];
+    if (wave == 0) {
+      const bool counts = r0 + lane < q1 && fabsf(held_lse) < INFINITY;     // a query whose lse is not finite counts nothing
+      tile_lse[buf][lane] = counts ? held_lse * 1.4426950408889634f : INFINITY;
+      const bool all = __builtin_amdgcn_ballot_w64(counts) == ~0ull;
+      if (lane == 0) tile_whole[buf] = all;
     }
   };
-  auto put = [&](int buf) {
+  // The block whose scores are there but whose exponentials are not taken yet: they go between the next block's matrix instructions.
+  f32x16 s[2];
+  float pending = 0.f;
 #pragma unroll
-    for (int x = 0; x < kLoads; ++x) {
-      const int piece = tid + kThreads * x, r = piece / PPR;
-      *reinterpret_cast<u32x4*>(&tile[buf][r * kRow + 16 * ((piece % PPR) ^ swizzle(r))]) = held[x];
+  for (int y = 0; y < 16; ++y) s[1][y] = -INFINITY;
+  auto mma = [](const u32x4& a, const u32x4& b, const f32x16& acc) {
+    if constexpr (sizeof(T) == 2) {
+      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+    } else {
+      f32x16 r = acc;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(b[e]), r, 0, 0, 0);
+      return r;
     }
-    if (tid < kTileRows) tile_lse[buf][tid] = held_lse;
   };
-  if (tiles > 0) { request(0); put(0); }
+  const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  auto load_q = [&](int buf, int half, u32x4 (&qf)[KP], float& l2) {
+    const int r = 32 * half + c;
+    l2 = tile_lse[buf][r];
+#pragma unroll
+    for (int p = 0; p < KP; ++p) qf[p] = *reinterpret_cast<const u32x4*>(&tile[buf][r * kRow + 16 * ((2 * p + hb) ^ swizzle(r))]);
+  };
+  request(0, q0);
+  put(0, q0);
   __syncthreads();
-  for (int i = 0; i < tiles; ++i) {
-    const int buf = i & 1;
-    if (i + 1 < tiles) request(i + 1);
-    const int r0 = q0 + (i % per_head) * kTileRows;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int i0 = r0 + 32 * half, r = 32 * half + c;
-      // no query, no key, all queries before the wave's keys, or all keys out of their windows
-      if (i0 >= q1 || my0 >= n || i0 + 31 < my0 || i0 - (my0 + 32 * KB - 1) >= P.window) continue;
-      const float l2 = tile_lse[buf][r];
-      const bool dead = !(l2 < INFINITY);
+  int g = 0, r0 = q0;
+  for (int buf = 0; g < G; buf ^= 1) {
+    const bool wraps = r0 + kTileRows >= q1;
+    const int g_next = wraps ? g + 1 : g, r_next = wraps ? q0 : r0 + kTileRows;
+    if (g_next < G) request(g_next, r_next);
+    // every query of the tile counts and sees every key of the wave
+    const bool plain = tile_whole[buf] && r0 >= my0 + 32 * KB - 1 && r0 + kTileRows - 1 - my0 < P.window && my0 < n;
+    if (plain) {
       u32x4 qf[KP];
+      float l2 = 0.f, l_old = pending;
 #pragma unroll
-      for (int p = 0; p < KP; ++p) qf[p] = *reinterpret_cast<const u32x4*>(&tile[buf][r * kRow + 16 * ((2 * p + hb) ^ swizzle(r))]);
-      if (__builtin_amdgcn_ballot_w64(dead)) {
-        if (dead)
-#pragma unroll
-          for (int p = 0; p < KP; ++p) qf[p] = u32x4{0u, 0u, 0u, 0u};
-      }
-#pragma unroll
-      for (int x = 0; x < KB; ++x) {
-        const int j0 = my0 + 32 * x;
-        f32x16 s;
-#pragma unroll
-        for (int y = 0; y < 16; ++y) s[y] = 0.f;
+      for (int st = 0; st < 2 * KB; ++st) {
+        const int half = st / KB, x = st % KB, now = st & 1, old = now ^ 1, xo = (st + KB * 2 - 1) % KB;
+        if (x == 0) load_q(buf, half, qf, l2);
+        s[now] = zero;
+        // the first matrix instruction goes before the exponentials that wait for the last one of the block before
 #pragma unroll
         for (int p = 0; p < KP; ++p) {
-          if constexpr (sizeof(T) == 2) {
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[x][p]), __builtin_bit_cast(bf16x8, qf[p]), s, 0, 0, 0);
-          } else {
+          s[now] = mma(kf[x][p], qf[p], s[now]);
+          if (p > 0)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[x][p][e]), __uint_as_float(qf[p][e]), s, 0, 0, 0);
-          }
+            for (int y = 16 * (p - 1) / (KP - 1); y < 16 * p / (KP - 1); ++y)
+              sum[xo][y] += __builtin_amdgcn_exp2f(fmaf(s[old][y], P.scale2, -l_old));
+          if constexpr (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
         }
-        const bool whole = i0 >= j0 + 31 && i0 + 31 - j0 < P.window;        // every query of the block sees every key
-        if (whole) {
+        l_old = l2;
+      }
+      pending = l2;
+    }
+    if (!plain && my0 < n) {
 #pragma unroll
-          for (int y = 0; y < 16; ++y) sum[x][y] += __builtin_amdgcn_exp2f(fmaf(s[y], P.scale2, -l2));
-        } else {
-          const int i_q = i0 + c;
+      for (int y = 0; y < 16; ++y) {
+        sum[KB - 1][y] += __builtin_amdgcn_exp2f(fmaf(s[1][y], P.scale2, -pending));
+        s[1][y] = -INFINITY;
+      }
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        const int i0 = r0 + 32 * half, i_q = i0 + c;
+        // no query, all queries before the wave's keys, or all keys out of their windows
+        if (i0 >= q1 || i0 + 31 < my0 || i0 - (my0 + 32 * KB - 1) >= P.window) continue;
+        u32x4 qf[KP];
+        float l2;
+        load_q(buf, half, qf, l2);
+        if (!(l2 < INFINITY))
+#pragma unroll
+          for (int p = 0; p < KP; ++p) qf[p] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int x = 0; x < KB; ++x) {
+          const int j0 = my0 + 32 * x;
+          f32x16 z = zero;
+#pragma unroll
+          for (int p = 0; p < KP; ++p) z = mma(kf[x][p], qf[p], z);
 #pragma unroll
           for (int y = 0; y < 16; ++y) {
             const int ago = i_q - (j0 + 8 * (y / 4) + 4 * hb + y % 4);
-            const float e = __builtin_amdgcn_exp2f(fmaf(s[y], P.scale2, -l2));
+            const float e = __builtin_amdgcn_exp2f(fmaf(z[y], P.scale2, -l2));
             sum[x][y] += ago >= 0 && ago < P.window ? e : 0.f;
           }
         }
       }
+      pending = 0.f;
     }
-    if (i + 1 < tiles) put(buf ^ 1);
+    if (g_next < G) put(buf ^ 1, r_next);
     __syncthreads();
+    g = g_next;
+    r0 = r_next;
   }
-  float* to = sums + ((int64_t)part * P.Hkv + h) * P.total + lo;
+#pragma unroll
+  for (int y = 0; y < 16; ++y) sum[KB - 1][y] += __builtin_amdgcn_exp2f(fmaf(s[1][y], P.scale2, -pending));
 #pragma unroll
   for (int x = 0; x < KB; ++x)
 #pragma unroll
@@ -177,13 +234,13 @@ mass_parts_kernel(const float* __restrict__ sums, int parts, int64_t n, float* _
 }
 
 struct Split { int parts, rows; };
+constexpr int64_t kFill = 2048;
 // Parts of the queries: as many as fill the chip a few times over, at most 2048 queries each.
 Split split_of(const ltea_cfg& cfg, const SeqView& sv, int last) {
-  const int64_t keys = cfg.dtype == LTEA_F32 ? kTileKeys<float> : kTileKeys<bf16_t>;
+  const int64_t keys = tile_keys(cfg);
   const int64_t groups = (sv.total_tokens / keys + 1) * cfg.Hkv;
-  int64_t reach = cfg.window + keys - 1 < sv.max_seqlen ? cfg.window + keys - 1 : sv.max_seqlen;
-  if (last > 0 && last < reach) reach = last;
-  int64_t parts = (1024 + groups - 1) / groups;
+  const int64_t reach = last > 0 && last < sv.max_seqlen ? last : sv.max_seqlen;
+  int64_t parts = (kFill + groups - 1) / groups;
   if (parts < (reach + 2047) / 2048) parts = (reach + 2047) / 2048;
   int64_t rows = ((reach + parts - 1) / parts + kTileRows - 1) / kTileRows * kTileRows;
   return Split{(int)((reach + rows - 1) / rows), (int)rows};
@@ -197,14 +254,15 @@ size_t mass_workspace(const ltea_cfg& cfg, const SeqView& sv, int last) {
 }
 // Of any call of up to so many tokens: a part for every 2048 queries of the longest sequence and one more, or as many as fill the chip.
 size_t mass_workspace_most(const ltea_cfg& cfg, int64_t total, int32_t max_seqlen) {
-  const size_t keys = cfg.dtype == LTEA_F32 ? kTileKeys<float> : kTileKeys<bf16_t>;
-  return (1024 * keys + (size_t)cfg.Hkv * total * (2 + (size_t)max_seqlen / 2048)) * sizeof(float);
+  const size_t keys = tile_keys(cfg);
+  return (kFill * keys + (size_t)cfg.Hkv * total * (2 + (size_t)max_seqlen / 2048)) * sizeof(float);
 }
 
-// The grid is a 32-bit number.
-bool mass_supported(const ltea_cfg& cfg, const SeqView& sv, int last) {
-  const int64_t keys = cfg.dtype == LTEA_F32 ? kTileKeys<float> : kTileKeys<bf16_t>;
-  return sv.total_tokens == 0 || (sv.total_tokens / keys + sv.n_seqs) * cfg.Hkv * split_of(cfg, sv, last).parts <= INT32_MAX;
+// The grid and the offsets inside a tile of queries are 32-bit numbers.
+bool mass_supported(const ltea_cfg& cfg, const SeqView& sv, int64_t q_st, int last) {
+  if (q_st * (cfg.dtype == LTEA_F32 ? 4 : 2) * kTileRows >= (int64_t)1 << 31) return false;
+  const int64_t keys = tile_keys(cfg);
+  return sv.total_tokens == 0 || (sv.total_tokens / keys + sv.n_seqs) * ((int64_t)cfg.Hkv * split_of(cfg, sv, last).parts + 7) <= INT32_MAX;
 }
 
 hipError_t launch_attention_mass(const ltea_cfg& cfg, const void* q, int64_t q_st, int64_t q_sh, const void* k, int64_t k_st, int64_t k_sh,
@@ -219,8 +277,9 @@ hipError_t launch_attention_mass(const ltea_cfg& cfg, const void* q, int64_t q_s
   auto go = [&](auto tag, auto dim) {
     using T = decltype(tag);
     constexpr int D = decltype(dim)::value;
-    P.tiles_upper = (int)(sv.total_tokens / kTileKeys<T> + sv.n_seqs);
-    hipLaunchKernelGGL((attention_mass_kernel<T, D>), dim3((unsigned)((int64_t)P.tiles_upper * cfg.Hkv * s.parts)), dim3(kThreads), 0,
+    P.tiles_upper = (int)(sv.total_tokens / kTileKeys<T, D> + sv.n_seqs);
+    P.units = cfg.Hkv * s.parts;
+    hipLaunchKernelGGL((attention_mass_kernel<T, D>), dim3((unsigned)((int64_t)P.tiles_upper * ((P.units + 7) / 8 * 8))), dim3(kThreads), 0,
                        stream, static_cast<const T*>(q), q_st, q_sh, static_cast<const T*>(k), k_st, k_sh, sv.cu_seqlens, lse, P, sums);
     return hipGetLastError();
   };

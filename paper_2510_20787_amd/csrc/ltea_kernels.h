@@ -160,7 +160,7 @@ hipError_t launch_decode_step_lazy(const ltea_cfg& cfg, const void* q, const voi
 // ---- weights of a prompt, the step that evicts by them, kept rows in 4 bits (attention_mass.hip, kept.hip) --------------------
 size_t mass_workspace(const ltea_cfg& cfg, const SeqView& sv, int last);
 size_t mass_workspace_most(const ltea_cfg& cfg, int64_t total, int32_t max_seqlen);      // of any call of up to so many tokens
-bool mass_supported(const ltea_cfg& cfg, const SeqView& sv, int last);
+bool mass_supported(const ltea_cfg& cfg, const SeqView& sv, int64_t q_stride_tok, int last);
 hipError_t launch_attention_mass(const ltea_cfg& cfg, const void* q, int64_t q_stride_tok, int64_t q_stride_head, const void* k,
                                  int64_t k_stride_tok, int64_t k_stride_head, const SeqView& sv, const float* lse, int last,
                                  float* mass, void* workspace, hipStream_t stream);
