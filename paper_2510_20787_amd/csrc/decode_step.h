@@ -162,26 +162,6 @@ template <typename V> __device__ __forceinline__ V load_uniform(const V* p) {
 }
 template <typename V> __device__ __forceinline__ void read_here(V& x) { asm volatile("" : "+s"(x)); }
 
-// Smallest value over the wave, in all lanes, on the cross-lane paths of the vector ALU: six steps of a few instructions where
-// LDS permutes would cost about 100 clocks each.
-__device__ __forceinline__ unsigned long long wave_min_u64(unsigned long long x) {
-  auto step = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
-    constexpr int kCtrl = decltype(ctrl)::value, kRows = decltype(rows)::value;
-    const uint32_t lo = __builtin_amdgcn_update_dpp(~0u, (uint32_t)x, kCtrl, kRows, 0xf, false);
-    const uint32_t hi = __builtin_amdgcn_update_dpp(~0u, (uint32_t)(x >> 32), kCtrl, kRows, 0xf, false);
-    const unsigned long long o = (unsigned long long)hi << 32 | lo;
-    x = o < x ? o : x;
-  };
-  step(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // row_shr:1
-  step(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});   // row_shr:2
-  step(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});   // row_shr:4
-  step(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});   // row_shr:8
-  step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast:15 into rows 1 and 3
-  step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // row_bcast:31 into rows 2 and 3
-  return (unsigned long long)__builtin_amdgcn_readlane((uint32_t)(x >> 32), kWave - 1) << 32 |
-         (uint32_t)__builtin_amdgcn_readlane((uint32_t)x, kWave - 1);
-}
-
 // A thread's first entries of a head's compact segment, requested before it is known whether they are needed.
 constexpr int kHeldKeys = 2;
 struct HeldKeys { float score[kHeldKeys]; int pos[kHeldKeys]; };

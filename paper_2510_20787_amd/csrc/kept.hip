@@ -141,7 +141,8 @@ size_t kept_workspace_most(const ltea_cfg& cfg, int n_seqs) {
 
 bool kept_step_supported(const ltea_cfg& cfg, int n_seqs) {
   if (cfg.Hq / cfg.Hkv > kKeptMaxGroup) return false;
-  if (cfg.window > (1 << 30) || cfg.budget > (1 << 30)) return false;
+  // a head's scores are addressed by 32-bit offsets
+  if (((int64_t)kept_blocks_of(cfg.window) + kept_blocks_of(cfg.budget)) * 128 * (cfg.Hq / cfg.Hkv) >= (int64_t)1 << 31) return false;
   return (int64_t)n_seqs * cfg.Hkv <= ((int64_t)1 << 24);
 }
 

@@ -10,19 +10,22 @@ struct KeptInputs { const void *q, *k, *v; void* out; const void* packed; int32_
 constexpr int kKeptMaxShares = 64;       // lanes of a wave
 constexpr int kKeptMaxGroup = 128;       // query heads per KV head
 
+constexpr size_t kKeptScoresLds = 40 * 1024;    // bytes of a head's scores that stay in LDS
+constexpr size_t kKeptLastShare = 16 * 1024;    // scores of a head that the last share to arrive takes on
+
 // What the workgroups of a head hand to the finishing launch, in floats of the workspace.
 struct KeptLayout {
   int G, D, nsplit, slots;
   // per head: t, count, bits of the leaving token's key, late; scores of the incoming and of the leaving token [2][G]; V row of the
   // leaving token as it would be kept [D]
   __host__ __device__ size_t plan() const { return 4 + 2 * (size_t)G + D; }
-  // per share: its lowest entry (key, position, slot, pad), that entry's scores [G], maximum, sum and output [G][D + 2]
-  __host__ __device__ size_t share() const { return 4 + (size_t)G + (size_t)G * (D + 2); }
+  // per share: its lowest entry (its place in the order, two words, slot, pad), that entry's scores [G] and V row [D], maximum, sum and output [G][D + 2]
+  __host__ __device__ size_t share() const { return 4 + (size_t)G + D + (size_t)G * (D + 2); }
   // per head: the scores of all slots [G][slots]
   __host__ __device__ size_t scores() const { return (size_t)G * slots; }
 };
 
-inline int kept_blocks_of(int rows) { return (rows + 31) / 32; }
+inline int kept_blocks_of(int rows) { return (int)(((int64_t)rows + 31) / 32); }
 
 #define LTEA_KEPT_RUN(name)                                                                                       \
   hipError_t name(const ltea_cfg& cfg, const KeptInputs& in, const ltea_cache& c, int n_seqs, int nsplit, void* workspace, \
