@@ -153,15 +153,6 @@ template <> struct Piece<bf16_t> {
   }
 };
 
-// A word that no workgroup changes before all that read it are done with it, through the scalar cache: such a load is not one of
-// the vector loads, which return in order, so waiting for it does not wait for rows requested earlier.  read_here: its memory
-// changes later, so the value is taken here, once.
-template <typename V> __device__ __forceinline__ V load_uniform(const V* p) {
-  static_assert(sizeof(V) == 4, "one word");
-  return __builtin_bit_cast(V, *reinterpret_cast<const __attribute__((address_space(4))) uint32_t*>(reinterpret_cast<uintptr_t>(p)));
-}
-template <typename V> __device__ __forceinline__ void read_here(V& x) { asm volatile("" : "+s"(x)); }
-
 // A thread's first entries of a head's compact segment, requested before it is known whether they are needed.
 constexpr int kHeldKeys = 2;
 struct HeldKeys { float score[kHeldKeys]; int pos[kHeldKeys]; };

@@ -1,4 +1,5 @@
 // Launchers of the step over kept entries (kept_step.h), and the conversion of kept rows to 4 bits and back.
+#include <initializer_list>
 #include "fp4_rows.h"
 #include "kept_run.h"
 
@@ -103,18 +104,25 @@ kept_unpack_kernel(const uint8_t* __restrict__ packed, const int32_t* __restrict
   }
 }
 
-// Shares of a head's rows (a workgroup of four waves each).
-int64_t shares_by_rows(const ltea_cfg& cfg, bool packed) {
+// Workgroups (shares) of a head and their waves.  A launch takes 256 CUs.
+// More heads than CUs: a head's workgroup of four waves, several of them on a CU (1024 heads of 1024 + 512 rows, D = 128: 136 us, with
+// eight waves 156; 512 heads of packed rows 86 and 99).  As many or fewer: eight waves (256 heads of 512 + 8192 packed rows, D = 128:
+// 73 us, with four 85).
+// Few heads of 64 blocks of rows or more are cut: 8 heads of 768 + 16384 packed rows 23 us in 16 shares, 75 whole.  The second launch
+// costs about 3 us and reading the shares grows with them: 8 heads of 768 + 512 rows 16.5 us whole, 18 in 3, 5 or 8 shares; 8 of
+// 768 + 32768 packed 35, 32, 32, 31, 38 and 47 us in 12, 16, 24, 32, 40 and 64; and where a head gets fewer than four CUs packed rows
+// do not gain (128 heads of 1024 + 8192: 46 us whole, 54 and 49 in 2 and 3), stored ones do (128 of 1024 + 2048: 58 whole, 46 in 2).
+constexpr int64_t kCus = 256;
+KeptSplit split_of(const ltea_cfg& cfg, int n_seqs, bool packed) {
+  const int64_t heads = (int64_t)n_seqs * cfg.Hkv, G = cfg.Hq / cfg.Hkv, fill = kCus / heads;
+  if (fill < 1) return KeptSplit{1, 4};
   const int64_t row = 2 * cfg.D * (cfg.dtype == LTEA_F32 ? 4 : 2), kept = packed ? 2 * (cfg.D / 2 + cfg.D / 32) : row;
-  const int64_t by_bytes = (cfg.window * row + cfg.budget * kept) / (64 * 1024);
-  const int64_t by_blocks = (kept_blocks_of(cfg.window) + kept_blocks_of(cfg.budget)) / 4;
-  const int64_t n = by_bytes < by_blocks ? by_bytes : by_blocks;
-  return n < 1 ? 1 : n > kKeptMaxShares ? kKeptMaxShares : n;
-}
-constexpr int64_t kKeptWorkgroups = 512;
-int kept_shares(const ltea_cfg& cfg, int n_seqs, bool packed) {
-  const int64_t heads = (int64_t)n_seqs * cfg.Hkv, n = shares_by_rows(cfg, packed), fill = kKeptWorkgroups / heads;
-  return (int)(fill < 1 ? 1 : n < fill ? n : fill);
+  const int64_t blocks = (int64_t)kept_blocks_of(cfg.window) + kept_blocks_of(cfg.budget), bytes = cfg.window * row + cfg.budget * kept;
+  if (blocks < 64 || fill < (packed ? 4 : 2)) return KeptSplit{1, 8};
+  const int64_t by_bytes = bytes / (256 * 1024), most = by_bytes < 16 ? 16 : by_bytes, by_lds = kKeptMaxFactors / G;
+  int64_t n = blocks / 10;
+  for (const int64_t limit : {fill, most, by_lds, (int64_t)kKeptMaxShares}) n = n < limit ? n : limit;
+  return KeptSplit{(int)n, 4};
 }
 
 size_t kept_floats(const ltea_cfg& cfg, int64_t heads, int64_t shares) {
@@ -131,12 +139,11 @@ size_t kept_packed_bytes(const ltea_cfg& cfg, int n_seqs) {
 
 size_t kept_workspace(const ltea_cfg& cfg, int n_seqs, bool packed) {
   const int64_t heads = (int64_t)n_seqs * cfg.Hkv;
-  return heads == 0 ? 0 : kept_floats(cfg, heads, heads * kept_shares(cfg, n_seqs, packed)) * sizeof(float);
+  return heads == 0 ? 0 : kept_floats(cfg, heads, heads * split_of(cfg, n_seqs, packed).shares) * sizeof(float);
 }
-size_t kept_workspace_most(const ltea_cfg& cfg, int n_seqs) {
-  const int64_t heads = (int64_t)n_seqs * cfg.Hkv, by_rows = heads * shares_by_rows(cfg, false);
-  const int64_t shared = by_rows < kKeptWorkgroups ? by_rows : kKeptWorkgroups;
-  return heads == 0 ? 0 : kept_floats(cfg, heads, shared > heads ? shared : heads) * sizeof(float);
+size_t kept_workspace_most(const ltea_cfg& cfg, int n_seqs) {      // with and without packed rows, and not less for more sequences
+  const int64_t heads = (int64_t)n_seqs * cfg.Hkv;
+  return heads == 0 ? 0 : kept_floats(cfg, heads, heads > kCus ? heads : kCus) * sizeof(float);
 }
 
 bool kept_step_supported(const ltea_cfg& cfg, int n_seqs) {
@@ -149,7 +156,7 @@ bool kept_step_supported(const ltea_cfg& cfg, int n_seqs) {
 hipError_t launch_kept_step(const ltea_cfg& cfg, const void* q, const void* k, const void* v, void* out, const ltea_cache& c,
                             const void* packed, bool mass, int n_seqs, int32_t* status, void* workspace, hipStream_t stream) {
   const KeptInputs in{q, k, v, out, packed, status, mass};
-  const int n = kept_shares(cfg, n_seqs, packed != nullptr);
+  const KeptSplit n = split_of(cfg, n_seqs, packed != nullptr);
   if (cfg.dtype == LTEA_F32)
     return cfg.D == 64 ? kept_run_f32_64(cfg, in, c, n_seqs, n, workspace, stream)
                        : kept_run_f32_128(cfg, in, c, n_seqs, n, workspace, stream);

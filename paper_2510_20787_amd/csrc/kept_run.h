@@ -10,8 +10,11 @@ struct KeptInputs { const void *q, *k, *v; void* out; const void* packed; int32_
 constexpr int kKeptMaxShares = 64;       // lanes of a wave
 constexpr int kKeptMaxGroup = 128;       // query heads per KV head
 
+constexpr int kKeptMaxFactors = 6144;    // query heads times shares: two numbers each in the second launch's LDS
 constexpr size_t kKeptScoresLds = 40 * 1024;    // bytes of a head's scores that stay in LDS
-constexpr size_t kKeptLastShare = 16 * 1024;    // scores of a head that the last share to arrive takes on
+constexpr size_t kKeptLds = 52 * 1024;          // bytes of LDS that a workgroup asks for beside its fixed arrays
+
+struct KeptSplit { int shares, waves; };        // of a head; waves of a workgroup that takes a whole one
 
 // What the workgroups of a head hand to the finishing launch, in floats of the workspace.
 struct KeptLayout {
@@ -28,7 +31,7 @@ struct KeptLayout {
 inline int kept_blocks_of(int rows) { return (int)(((int64_t)rows + 31) / 32); }
 
 #define LTEA_KEPT_RUN(name)                                                                                       \
-  hipError_t name(const ltea_cfg& cfg, const KeptInputs& in, const ltea_cache& c, int n_seqs, int nsplit, void* workspace, \
+  hipError_t name(const ltea_cfg& cfg, const KeptInputs& in, const ltea_cache& c, int n_seqs, KeptSplit split, void* workspace, \
                   hipStream_t stream)
 LTEA_KEPT_RUN(kept_run_f32_64);
 LTEA_KEPT_RUN(kept_run_f32_128);

@@ -11,13 +11,11 @@
 // Two rows are left out of the stream, because what is at their place differs before and after the step: the ring slot t % window,
 // and the entry that e displaces.  What replaces them, e as it would be kept and the incoming token, joins the softmax at the end;
 // with the normaliser known every key of the head grows by its weight, and the rows move.
-// Where heads are few, a head is cut into shares.  No share knows the lowest entry of all then, so each leaves out its own lowest
-// when e may displace one, and hands its score and value row on beside its maximum, sum and output: whoever finishes the head adds
-// those that stay.  That is the share that arrives last, or a second launch whose workgroups add the weights to a share each
-// (launches of very long heads, and caches whose counts do not fit, see below).
-// Arrivals are counted in the upper bits of ret_count as ltea_decode_step does it (bits 16..23 of a head's word its shares, bits
-// 24..31 of a sequence's first word its heads), handed-over words go past the XCD's own L2 (agent scope), and nobody waits for
-// anybody.
+// Where heads are few and long, a head is cut into shares and a second launch finishes it.  No share knows the lowest entry of all
+// then, so each leaves out its own lowest when e may displace one, and hands its score and value row on beside its maximum, sum and
+// output; the second launch adds those that stay, and each of its workgroups the weights of a share's entries.
+// A whole head's workgroup counts itself in bits 24..31 of its sequence's first word of ret_count, as ltea_decode_step does, and the
+// last one advances the sequence's counters.  Caches whose counts do not fit there take the two launches.
 //
 //   S^T[row, head] = K . Q^T       v_mfma_f32_16x16x32_bf16; K rows straight from memory into the A operand
 //   O^T[d, head] += V^T . P^T      V in registers, eight rows of a few channels per lane, brought into the A operand's order by
@@ -29,15 +27,15 @@
 #pragma once
 #include "fp4_rows.h"
 #include "kept_run.h"
+#include "score_dma.h"
 
 namespace ltea {
 namespace {
 
-constexpr int kStepWaves = 4, kStepThreads = kStepWaves * kWave;
+constexpr int kStepWaves = 4, kStepThreads = kStepWaves * kWave;     // of a workgroup that shares a head, and of the second launch
 
 struct KeptParams {
   int B, Hq, Hkv, window, budget, sink, mass;
-  int fused;                     // the head is finished in the first launch
   int scores_in_lds;
   uint32_t count_mask;           // the bits of ret_count that are the count
   float tau, scale2;             // scale * log2(e)
@@ -80,7 +78,7 @@ __device__ __forceinline__ auto bytes_at(const void* p, uint32_t bytes) {
                                        (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a));
   return __builtin_amdgcn_make_buffer_rsrc(same, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
 }
-constexpr int kNonTemporal = 2, kPastL2 = 16;              // of buffer instructions
+constexpr int kNonTemporal = 2;              // of buffer instructions
 
 // ---- 32 rows of a head in registers ------------------------------------------------------------------------------------------
 // Stored rows.  K: piece i of tile j is 16 bytes of row 8 (c / 4) + 4 j + c % 4 of the block.  V: row 8 kg + u, a lane's channels
@@ -160,10 +158,11 @@ template <int D> struct PackedRows {
   }
   // codes of K tile j, eight channels i
   __device__ __forceinline__ uint32_t k_codes(int j, int i) const { return D == 128 ? k[j][i] : k[0][2 * j + i]; }
-  __device__ __forceinline__ float k_scale(int j) const { return group_scale(ke >> (8 * j) & 255u); }
+  // 2^E as the conversion takes it: it reads the exponent bits, and gives NaN for 255
+  __device__ __forceinline__ float k_scale(int j) const { return __uint_as_float((ke >> (8 * j) & 255u) << 23); }
   // codes of V row u: D = 128 a word, D = 64 the lower half of one
   __device__ __forceinline__ uint32_t v_codes(int u) const { return D == 128 ? v[u >> 2][u & 3] : v[0][u >> 1] >> (16 * (u & 1)); }
-  __device__ __forceinline__ float v_scale(int u) const { return group_scale(ve[u >> 2] >> (8 * (u & 3)) & 255u); }
+  __device__ __forceinline__ float v_scale(int u) const { return __uint_as_float((ve[u >> 2] >> (8 * (u & 3)) & 255u) << 23); }
   __device__ __forceinline__ void clear(uint32_t dead) {
 #pragma unroll
     for (int u = 0; u < 8; ++u)
@@ -186,33 +185,50 @@ __device__ __forceinline__ uint32_t bf16_pair(uint32_t codes, float scale, int b
   return __builtin_bit_cast(uint32_t, r);
 }
 
-// ---- scores and outputs of 32 rows --------------------------------------------------------------------------------------------
-// Scores x[u] of row 8 kg + u against the lane's column.  qf: the column's query in the channel order of the rows.
-template <int D> __device__ __forceinline__ void score_rows(const StoredRows<bf16_t, D>& R, const bf16x8 (&qf)[D / 32], float (&x)[8]) {
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, R.k[j][i]), qf[i], acc, 0, 0, 0);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) x[4 * j + r] = acc[r];
+// The same as two fp32 values.
+__device__ __forceinline__ void f32_pair(uint32_t codes, float scale, int byte, float& a, float& b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  f32x2 r;
+  switch (byte) {
+    case 0: r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0); break;
+    case 1: r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1); break;
+    case 2: r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2); break;
+    default: r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3); break;
   }
+  a = r[0];
+  b = r[1];
 }
-template <int D> __device__ __forceinline__ void score_rows(const PackedRows<D>& R, const bf16x8 (&qf)[D / 32], float (&x)[8]) {
+
+// ---- scores and outputs of 32 rows --------------------------------------------------------------------------------------------
+// Scores x[u] of row 8 kg + u against the lane's column.  qf: the column's query in the channel order of the rows; bf16: in LDS, this
+// lane's piece i at qf[64 * i] (16 registers less for as many bytes read per block as two rows have).
+template <int D> __device__ __forceinline__ void score_rows(const StoredRows<bf16_t, D>& R, const u32x4* qf, float (&x)[8]) {
+  f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    const float sc = R.k_scale(j);
+  for (int i = 0; i < D / 32; ++i) {
+    const bf16x8 b = __builtin_bit_cast(bf16x8, qf[64 * i]);
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
+    for (int j = 0; j < 2; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, R.k[j][i]), b, acc[j], 0, 0, 0);
+  }
+#pragma unroll
+  for (int u = 0; u < 8; ++u) x[u] = acc[u >> 2][u & 3];
+}
+template <int D> __device__ __forceinline__ void score_rows(const PackedRows<D>& R, const u32x4* qf, float (&x)[8]) {
+  f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  const float sc[2] = {R.k_scale(0), R.k_scale(1)};
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    const bf16x8 b = __builtin_bit_cast(bf16x8, qf[64 * i]);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
       u32x4 a;
 #pragma unroll
-      for (int p = 0; p < 4; ++p) a[p] = bf16_pair(R.k_codes(j, i), sc, p);
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), qf[i], acc, 0, 0, 0);
+      for (int p = 0; p < 4; ++p) a[p] = bf16_pair(R.k_codes(j, i), sc[j], p);
+      acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), b, acc[j], 0, 0, 0);
     }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) x[4 * j + r] = acc[r];
   }
+#pragma unroll
+  for (int u = 0; u < 8; ++u) x[u] = acc[u >> 2][u & 3];
 }
 template <int D> __device__ __forceinline__ void score_rows(const StoredRows<float, D>& R, const float (&qf)[D / 4], float (&x)[8]) {
 #pragma unroll
@@ -235,8 +251,12 @@ template <int D> __device__ __forceinline__ void score_rows(const PackedRows<D>&
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(code_value(R.k_codes(j, i) >> (4 * e), sc), qf[8 * i + e], acc, 0, 0, 0);
+      for (int e = 0; e < 8; e += 2) {
+        float a0, a1;
+        f32_pair(R.k_codes(j, i), sc, e / 2, a0, a1);
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a0, qf[8 * i + e], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a1, qf[8 * i + e + 1], acc, 0, 0, 0);
+      }
 #pragma unroll
     for (int r = 0; r < 4; ++r) x[4 * j + r] = acc[r];
   }
@@ -286,8 +306,12 @@ template <int D> __device__ __forceinline__ void add_values(const PackedRows<D>&
   for (int u = 0; u < 8; ++u) {
     const float sc = R.v_scale(u);
 #pragma unroll
-    for (int n = 0; n < D / 16; ++n)
-      o[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(code_value(R.v_codes(u) >> (4 * n), sc), p[u], o[n], 0, 0, 0);
+    for (int n = 0; n < D / 16; n += 2) {
+      float a0, a1;
+      f32_pair(R.v_codes(u), sc, n / 2, a0, a1);
+      o[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a0, p[u], o[n], 0, 0, 0);
+      o[n + 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(a1, p[u], o[n + 1], 0, 0, 0);
+    }
   }
 }
 
@@ -304,14 +328,14 @@ template <typename T, int D, int GT> struct Running {
 #pragma unroll
     for (int n = 0; n < D / 16; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  // x: scores in log2 units, -inf where the row does not count
-  template <typename R> __device__ __forceinline__ void add(const R& rows, const float (&x)[8], bool second_term) {
+  // x: q . k, -inf where the row does not count; scale2: softmax scale in log2 units (positive)
+  template <typename R> __device__ __forceinline__ void add(const R& rows, const float (&x)[8], float scale2, bool second_term) {
     float top = x[0];
 #pragma unroll
     for (int u = 1; u < 8; ++u) top = fmaxf(top, x[u]);
     const float m_new = fmaxf(m, column_max(top));
     if (__builtin_amdgcn_ballot_w64(m_new > m)) {
-      const float f = m == -INFINITY ? 0.f : exp2_hw(m - m_new);
+      const float f = m == -INFINITY ? 0.f : exp2_hw((m - m_new) * scale2);
       l *= f;
 #pragma unroll
       for (int n = 0; n < D / 16; ++n)
@@ -319,28 +343,30 @@ template <typename T, int D, int GT> struct Running {
         for (int r = 0; r < 4; ++r) o[n][r] *= f;
       m = m_new;
     }
-    const float ref = m == -INFINITY ? 0.f : m;      // no row so far
+    const float ref = m == -INFINITY ? 0.f : m * scale2;      // no row so far
     float p[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      p[u] = exp2_hw(x[u] - ref);
+      p[u] = exp2_hw(fmaf(x[u], scale2, -ref));
       l += p[u];
     }
     if constexpr (sizeof(T) == 4) {
       add_values(rows, p, o);
     } else {
-      bf16x8 hi, t[kTerms];
+      u32x4 first, rest;               // the bf16 values, two to a word, and those of what they leave
+      const float take = kTermColumns && !second_term ? 0.f : 1.f;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) hi[u] = (bf16_t)p[u];
-      if constexpr (kTermColumns) {
-        const float take = second_term ? 1.f : 0.f;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) t[0][u] = (bf16_t)fmaf(-take, (float)hi[u], p[u]);
-      } else {
-        t[0] = hi;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) t[kTerms - 1][u] = (bf16_t)(p[u] - (float)hi[u]);
+      for (int w = 0; w < 4; ++w) {
+        const bf16x2 hi = {(bf16_t)p[2 * w], (bf16_t)p[2 * w + 1]};
+        first[w] = __builtin_bit_cast(uint32_t, hi);
+        const float lo0 = fmaf(-take, __uint_as_float(first[w] << 16), p[2 * w]);
+        const float lo1 = fmaf(-take, __uint_as_float(first[w] & 0xFFFF0000u), p[2 * w + 1]);
+        const bf16x2 lo = {(bf16_t)lo0, (bf16_t)lo1};
+        rest[w] = __builtin_bit_cast(uint32_t, lo);
       }
+      bf16x8 t[kTerms];
+      t[0] = __builtin_bit_cast(bf16x8, kTermColumns ? rest : first);
+      t[kTerms - 1] = __builtin_bit_cast(bf16x8, rest);
       add_values<D, kTerms>(rows, t, o);
     }
   }
@@ -395,20 +421,33 @@ __device__ __forceinline__ int target_of(const KeptParams& P, const Plan& p, con
   return __builtin_amdgcn_readfirstlane(dst);
 }
 
-// A word that another workgroup of this launch wrote, or one of an earlier launch.
-template <bool SHARED> __device__ __forceinline__ float take(const float* p) {
-  if constexpr (SHARED) return __hip_atomic_load(const_cast<float*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  else return *p;
-}
-__device__ __forceinline__ void give(float* p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-
 // The weights of entries join their keys, four rows per thread at a time, and the leaving token's key and position take their slot.
 // score4(g, at): scores of slots at .. at + 3 of [ring ++ kept] against query head g; a probability that is not a number counts as
 // nothing.  The rows are those of blocks sh.
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-template <typename F>
+// What a thread needs first of all, requested ahead: keys of its first rows of either segment and their scores against the first
+// four query heads.
+struct FirstRows { f32x4 ring, kept, x_ring[4], x_kept[4]; };
+__device__ __forceinline__ f32x4 keys_at(const float* keys, int n, int r) {       // of n keys; past them zeros
+  return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(bytes_at(keys, (uint32_t)n * 4u), (uint32_t)r * 4u, 0, 0));
+}
+__device__ __forceinline__ void request_keys(const CacheDev& C, const KeptParams& P, int64_t head, const Share& sh, FirstRows& F) {
+  if (!P.mass) return;
+  F.ring = keys_at(C.win_score + head * P.window, P.window, 32 * sh.ring0 + 4 * (int)threadIdx.x);
+  F.kept = keys_at(C.ret_score + head * P.budget, P.budget, 32 * sh.kept0 + 4 * (int)threadIdx.x);
+}
+template <typename F4> __device__ __forceinline__ void request_scores(const KeptParams& P, const Share& sh, FirstRows& F, F4&& score4) {
+  if (!P.mass) return;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int gc = g < P.L.G ? g : 0;
+    F.x_ring[g] = score4(gc, 32 * sh.ring0 + 4 * (int)threadIdx.x);
+    F.x_kept[g] = score4(gc, 32 * ((P.window + 31) / 32) + 32 * sh.kept0 + 4 * (int)threadIdx.x);
+  }
+}
+template <int NT, typename F4>
 __device__ __forceinline__ void grow_keys(const CacheDev& C, const KeptParams& P, const Plan& p, int64_t head, const Share& sh, int dst,
-                                          const float* xs, const float* top, const float* inv, F&& score4) {
+                                          const float* xs, const float* top, const float* inv, const FirstRows& first, bool have_scores,
+                                          F4&& score4) {
   const int G = P.L.G, tid = threadIdx.x;
   if (!P.mass) {
     if (dst >= 32 * sh.kept0 && dst < 32 * sh.kept1 && tid == 0) {
@@ -417,28 +456,28 @@ __device__ __forceinline__ void grow_keys(const CacheDev& C, const KeptParams& P
     }
     return;
   }
-  auto weight = [&](float x, int g) { return fmaxf(exp2_hw(x - top[g]) * inv[g], 0.f); };
-  // keys of rows r0 .. r1 of one segment; special: the row of the incoming (or leaving) token, whose key starts at `base`
-  auto grow = [&](float* keys, int r0, int r1, int at0, int special, float base, const float* special_x) {
-    for (int r = r0 + 4 * tid; r < r1; r += 4 * kStepThreads) {
-      float before[4], w[4] = {0.f, 0.f, 0.f, 0.f};
-      const bool all = r + 4 <= r1;
-      if (all) {
-        const f32x4_any x = *reinterpret_cast<const f32x4_any*>(keys + r);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) before[i] = x[i];
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) before[i] = keys[r + i < r1 ? r + i : r1 - 1];
-      }
+  auto weight = [&](float x, int g) { return fmaxf(exp2_hw(fmaf(x, P.scale2, -top[g])) * inv[g], 0.f); };
+  // keys of rows r0 .. r1 of one segment of n; special: the row of the incoming (or leaving) token, whose key starts at `base`
+  auto grow = [&](float* keys, int n, int r0, int r1, int at0, int special, float base, const float* special_x, const f32x4& first_keys,
+                  const f32x4 (&first_x)[4]) {
+    const auto to = bytes_at(keys, (uint32_t)n * 4u);
+    for (int r = r0 + 4 * tid; r < r1; r += 4 * NT) {
+      const bool is_first = r == r0 + 4 * tid;
+      f32x4 before = first_keys, w = {0.f, 0.f, 0.f, 0.f};
+      if (!is_first) before = keys_at(keys, n, r);
       for (int g0 = 0; g0 < G; g0 += 4) {
         f32x4 x[4];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) x[g] = score4(g0 + g < G ? g0 + g : g0, at0 + r);
+        for (int g = 0; g < 4; ++g) x[g] = first_x[g];
+        if (!(is_first && have_scores && g0 == 0)) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) x[g] = score4(g0 + g < G ? g0 + g : g0, at0 + r);
+        }
 #pragma unroll
         for (int g = 0; g < 4; ++g)
+          if (g0 + g < G)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] += g0 + g < G ? weight(x[g][i], g0 + g) : 0.f;
+            for (int i = 0; i < 4; ++i) w[i] += weight(x[g][i], g0 + g);
       }
       if (special >= r && special < r + 4) {
         float ws = 0.f;
@@ -447,19 +486,22 @@ __device__ __forceinline__ void grow_keys(const CacheDev& C, const KeptParams& P
         for (int i = 0; i < 4; ++i)
           if (r + i == special) { before[i] = base; w[i] = ws; }
       }
-      if (all) {
-        *reinterpret_cast<f32x4_any*>(keys + r) = f32x4_any{before[0] + w[0], before[1] + w[1], before[2] + w[2], before[3] + w[3]};
+      const f32x4 after = before + w;
+      if (r + 4 <= r1) {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, after), to, (uint32_t)r * 4u, 0, 0);
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (r + i < r1) keys[r + i] = before[i] + w[i];
+        for (int i = 0; i < 3; ++i)
+          if (r + i < r1) keys[r + i] = after[i];
       }
     }
   };
   const int live = p.t + 1 < P.window ? p.t + 1 : P.window;
-  grow(C.win_score + head * P.window, 32 * sh.ring0, 32 * sh.ring1 < live ? 32 * sh.ring1 : live, 0, p.slot, 0.f, xs);
+  grow(C.win_score + head * P.window, P.window, 32 * sh.ring0, 32 * sh.ring1 < live ? 32 * sh.ring1 : live, 0, p.slot, 0.f, xs,
+       first.ring, first.x_ring);
   const int after = p.count + (dst == p.count ? 1 : 0), k1 = 32 * sh.kept1 < after ? 32 * sh.kept1 : after;
-  grow(C.ret_score + head * P.budget, 32 * sh.kept0, k1, 32 * ((P.window + 31) / 32), dst, p.e_key, xs + G);
+  grow(C.ret_score + head * P.budget, P.budget, 32 * sh.kept0, k1, 32 * ((P.window + 31) / 32), dst, p.e_key, xs + G, first.kept,
+       first.x_kept);
   if (dst >= 32 * sh.kept0 && dst < k1 && tid == 0) C.ret_pos[head * P.budget + dst] = p.leaving;
 }
 
@@ -505,20 +547,21 @@ __device__ __forceinline__ void advance(const CacheDev& C, const KeptParams& P, 
 
 // What all shares of a head have handed over becomes factors: fac [G][n] of the shares' outputs, stay [G][n] weights of their lowest
 // entries that stay (both relative to 2^top), top [G], inv [G] = 1 / sum.  Returns the slot the leaving token goes to.
-template <bool SHARED, int D>
+template <int D>
 __device__ __forceinline__ int join_shares(const KeptParams& P, const Plan& p, const float* rec, const float* xs, float* fac, float* stay,
                                            float* top, float* inv) {
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const int n = P.L.nsplit, G = P.L.G;
   const float* r = rec + (lane < n ? lane : 0) * P.L.share();
-  Entry mine = {(unsigned long long)__float_as_uint(take<SHARED>(r)) << 32 | __float_as_uint(take<SHARED>(r + 1)), __float_as_int(take<SHARED>(r + 2))};
+  Entry mine = {(unsigned long long)__float_as_uint(r[0]) << 32 | __float_as_uint(r[1]), __float_as_int(r[2])};
   if (lane >= n) mine = Entry{~0ull, -1};
   const int dst = target_of(P, p, first_of_wave(mine));
   const bool stays = mine.slot >= 0 && mine.slot != dst;
   for (int g = wave; g < G; g += kStepWaves) {
     const float* o = r + 4 + G + D + (size_t)g * (D + 2);
-    const float m = lane < n ? take<SHARED>(o) : -INFINITY, l = lane < n ? take<SHARED>(o + 1) : 0.f;
-    const float x_s = stays ? take<SHARED>(r + 4 + g) : -INFINITY, x_t = xs[g], x_e = dst >= 0 ? xs[G + g] : -INFINITY;
+    const float m = lane < n ? o[0] : -INFINITY, l = lane < n ? o[1] : 0.f;
+    const float x_s = stays ? r[4 + g] * P.scale2 : -INFINITY, x_t = xs[g] * P.scale2;
+    const float x_e = dst >= 0 ? xs[G + g] * P.scale2 : -INFINITY;
     const float M = fmaxf(fmaxf(wave_max(fmaxf(m, x_s)), x_t), x_e);
     const float ref = M == -INFINITY ? 0.f : M;
     const float f = exp2_hw(m - ref), w_s = exp2_hw(x_s - ref);
@@ -529,55 +572,66 @@ __device__ __forceinline__ int join_shares(const KeptParams& P, const Plan& p, c
   return dst;
 }
 
-// Output element (g, d) of the head from all shares.
-template <bool SHARED, typename T, int D>
+// Output element (g, d) of the head from all shares, sixteen of them at a time; of the first sixteen what is handed over is requested
+// ahead.
+constexpr int kBatch = 16;
+struct FirstShares { float o[kBatch], v[kBatch]; };
+template <int D>
+__device__ __forceinline__ void take_shares(const KeptParams& P, const float* rec, int g, int d, int s0, FirstShares& F) {
+#pragma unroll
+  for (int u = 0; u < kBatch; ++u) {
+    const float* r = rec + (s0 + u < P.L.nsplit ? s0 + u : s0) * P.L.share() + 4 + P.L.G;
+    F.v[u] = r[d];
+    F.o[u] = r[D + (size_t)g * (D + 2) + 2 + d];
+  }
+}
+template <int D>
 __device__ __forceinline__ float joined_output(const KeptParams& P, const float* rec, int g, int d, int dst, const float* xs, float v_in,
-                                               float v_e, const float* fac, const float* stay, const float* top, const float* inv) {
+                                               float v_e, const float* fac, const float* stay, const float* top, const float* inv,
+                                               FirstShares& F) {
   const int n = P.L.nsplit, G = P.L.G;
-  float A = exp2_hw(xs[g] - top[g]) * v_in;
-  if (dst >= 0) A = fmaf(exp2_hw(xs[G + g] - top[g]), v_e, A);
-  constexpr int kBatch = 16;
-  for (int s0 = 0; s0 < n; s0 += kBatch) {
-    float o[kBatch], v[kBatch];
+  float A = exp2_hw(fmaf(xs[g], P.scale2, -top[g])) * v_in;
+  if (dst >= 0) A = fmaf(exp2_hw(fmaf(xs[G + g], P.scale2, -top[g])), v_e, A);
+  for (int s0 = 0;;) {
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      const float* r = rec + (s0 + u < n ? s0 + u : s0) * P.L.share() + 4 + G;
-      v[u] = take<SHARED>(r + d);
-      o[u] = take<SHARED>(r + D + (size_t)g * (D + 2) + 2 + d);
+      const bool there = s0 + u < n;
+      const int at = g * n + (there ? s0 + u : s0);
+      const float w = stay[at];
+      if (there) A = fmaf(F.o[u], fac[at], A);
+      if (there && w != 0.f) A = fmaf(w, F.v[u], A);        // (a row that does not stay may hold anything)
     }
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      if (s0 + u >= n) break;
-      A = fmaf(o[u], fac[g * n + s0 + u], A);
-      const float w = stay[g * n + s0 + u];
-      if (w != 0.f) A = fmaf(w, v[u], A);        // (a row that does not stay may hold anything)
-    }
+    s0 += kBatch;
+    if (s0 >= n) break;
+    take_shares<D>(P, rec, g, d, s0, F);
   }
   return A * inv[g];
 }
 
-// How a head is finished: by its one workgroup, by the last of its shares, or by the second launch.
-enum { kWhole, kLastShare, kSecondLaunch };
-
-template <typename T, int D, bool PK, int GT, int MODE>
-__global__ void __launch_bounds__(kStepThreads, sizeof(T) == 4 ? 2 : D == 128 ? (PK ? 2 : 3) : PK ? 3 : 4)
+// WHOLE: the workgroup takes a whole head and finishes it; otherwise a share, and a second launch finishes the head.
+// Bound: HBM for long or many heads, else the chain of requests, products and exchanges of one head.  Waves per SIMD: as many as hold
+// their registers; D = 128 with three spills (1024 heads of 1024 + 512 rows 148 us, with two 136; 256 heads of 512 + 8192 packed rows
+// 78 and 73).
+template <typename T, int D, bool PK, int GT, bool WHOLE, int W>
+__global__ void __launch_bounds__(W * kWave, sizeof(T) == 4 || D == 128 ? 2 : PK ? 3 : 4)
 kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __restrict__ k_new, const T* __restrict__ v_new,
                  T* __restrict__ out) {
   using S = StoredRows<T, D>;
-  constexpr int W = kStepWaves, kRow = D + 4, kDepth = sizeof(T) == 4 ? 1 : 3;      // kDepth: blocks of packed rows in flight per wave
+  constexpr int NT = W * kWave, kRow = D + 4, kDepth = sizeof(T) == 4 ? 1 : 3;      // kDepth: blocks of packed rows in flight per wave
   constexpr int kQ = sizeof(T) == 4 ? D / 4 : D / 32;
-  using Q = typename std::conditional<sizeof(T) == 4, float, bf16x8>::type;
   // [W][heads of a pass][kRow] outputs of the waves, [2][G] scores of the incoming and the leaving token, [G] top, [G] inv,
-  // [G] scores of the lowest entry, then the scores of all slots [G][slots], or the shares' factors [2][G][nsplit]
+  // [G] scores of the lowest entry, then the scores of all slots [G][slots]
   extern __shared__ __align__(16) float lds[];
   __shared__ float red_m[W][16], red_l[W][16];
   __shared__ Entry red_e[W];
   __shared__ float ve_lds[D];
-  __shared__ int last_lds;
+  __shared__ __align__(16) u32x4 q_lds[sizeof(T) == 2 ? (PK ? 2 : 1) * kQ * kWave : 1];      // bf16: a pass's queries as B operands, [rows, packed rows][piece][lane]
+  __shared__ __align__(16) T rows_lds[3][D];          // keys of the incoming and of the leaving token, the latter's value
+  static_assert(sizeof(red_m) + sizeof(red_l) + sizeof(red_e) + sizeof(ve_lds) + sizeof(q_lds) + sizeof(rows_lds) + kKeptLds <= 64 * 1024, "LDS");
   const int tid = threadIdx.x, lane = tid & (kWave - 1), c = lane & 15, kg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int n = MODE == kWhole ? 1 : P.L.nsplit, split = MODE == kWhole ? 0 : blockIdx.x % n, G = P.L.G;
-  const int64_t head = MODE == kWhole ? blockIdx.x : blockIdx.x / n;
+  const int n = WHOLE ? 1 : P.L.nsplit, split = WHOLE ? 0 : blockIdx.x % n, G = P.L.G;
+  const int64_t head = WHOLE ? blockIdx.x : blockIdx.x / n;
   const int b = (int)(head / P.Hkv), h = (int)(head - (int64_t)b * P.Hkv);
   const int heads_at_once = G < GT ? G : GT;
   float* red_o = lds;
@@ -595,7 +649,46 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
   float* rec = P.shares + (head * n + split) * P.L.share();
   float* scores = P.scores + head * P.L.scores();
 
-  // Requested before anything is known: the wave's first ring block, whatever it holds, and the first keys of the share.
+  // Requested before anything is known: the scalar words (scalar loads do not wait for rows requested earlier, vector loads return in
+  // order), the queries, the first keys of the share, and last the wave's first rows, whatever they hold.
+  const int col = Running<T, D, GT>::kTermColumns ? c & 7 : c;
+  const bool second = Running<T, D, GT>::kTermColumns && c >= 8;
+  constexpr int kSets = PK ? 2 : 1, kMine = (kSets * kQ + W - 1) / W;      // bf16: pieces of the queries that a wave brings into LDS
+  u32x4 q_piece[sizeof(T) == 2 ? kMine : 1];
+  auto query_row = [&](int g0) { return q + ((int64_t)b * P.Hq + h * G + (g0 + col < G ? g0 + col : 0)) * D; };
+  auto request_queries = [&](int g0) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        const int piece = wave + i * W, set = piece / kQ, at = piece % kQ;
+        const T* row = query_row(g0) + (set == 0 ? S::k_channel(at, kg, 0) : PackedRows<D>::k_channel(at, kg, 0));
+        q_piece[i] = *reinterpret_cast<const u32x4*>(row);
+      }
+    }
+  };
+  auto put_queries = [&](int g0) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < kMine; ++i)
+        if (wave + i * W < kSets * kQ) q_lds[(wave + i * W) * kWave + lane] = g0 + col < G ? q_piece[i] : u32x4{0u, 0u, 0u, 0u};
+    }
+  };
+  request_queries(0);
+  int t = load_uniform(C.n_seen + b), held = P.budget > 0 ? load_uniform(C.ret_count + head) : 0, scored = P.mass ? 0 : load_uniform(C.n_scored + b);
+  constexpr int kAhead = 2;
+  float key_ahead[kAhead];
+  int pos_ahead[kAhead];
+  const int key0 = 32 * sh.kept0 + tid, key1 = 32 * sh.kept1 < P.budget ? 32 * sh.kept1 : P.budget;
+  {
+    const uint32_t bytes = (uint32_t)(key1 > 0 ? key1 : 0) * 4u;
+    const auto rk = bytes_at(C.ret_score + head * P.budget, bytes), rp = bytes_at(C.ret_pos + head * P.budget, bytes);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {       // (no branches: they would be waited for at its end)
+      const uint32_t at = (uint32_t)(key0 + i * NT) * 4u;
+      key_ahead[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rk, at, 0, 0));
+      pos_ahead[i] = (int)__builtin_amdgcn_raw_buffer_load_b32(rp, at, 0, 0);
+    }
+  }
   S R;
   const int first_ring = sh.ring0 + wave;
   auto load_ring_k = [&](int blk, bool there) { R.load_k(kw + (int64_t)32 * blk * D, there ? P.window - 32 * blk : 0); };
@@ -611,26 +704,21 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
       K[i].load(blocks + (int64_t)blk * PackGeo<D>::kBlock, blk < sh.kept1);
     }
   };
-  if constexpr (PK) request_packed();
-  constexpr int kAhead = 2;
-  float key_ahead[kAhead];
-  int pos_ahead[kAhead];
-  const int key0 = 32 * sh.kept0 + tid, key1 = 32 * sh.kept1 < P.budget ? 32 * sh.kept1 : P.budget;
-#pragma unroll
-  for (int i = 0; i < kAhead; ++i) {
-    const int r = key0 + i * kStepThreads;
-    const bool there = r < key1;
-    key_ahead[i] = there ? C.ret_score[head * P.budget + r] : 0.f;
-    pos_ahead[i] = there ? C.ret_pos[head * P.budget + r] : 0;
+  if constexpr (PK && D == 64) request_packed();        // (D = 128: the registers are the ring's)
+  read_here(t);
+  read_here(held);
+  read_here(scored);
+  held = (int)((uint32_t)held & P.count_mask);
+  const int count = held < P.budget ? held : P.budget;
+  const bool late = !P.mass && t >= P.window && scored <= t - P.window;
+  float z_e = t >= P.window ? load_uniform(C.win_score + head * P.window + t % P.window) : 0.f;
+  read_here(z_e);
+  const Plan p = plan_of(P, t, count, z_e, late);
+  // rows that are needed at the end, straight into LDS
+  if (wave < 3 && lane < D * (int)sizeof(T) / 16) {
+    const T* row = wave == 0 ? k_new + head * D : (wave == 1 ? kw : vw) + (int64_t)p.slot * D;
+    dma16(make_raw_rsrc(row, (uint32_t)(D * sizeof(T))), (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)&rows_lds[wave][0], 16u * (uint32_t)lane);
   }
-  float x_in[D / 64], x_out[D / 64], v_out[D / 64];
-  load_kept_form<T, D, false>(k_new + head * D, x_in);
-  const int t = C.n_seen[b];
-  const int held = P.budget > 0 ? (int)((uint32_t)C.ret_count[head] & P.count_mask) : 0, count = held < P.budget ? held : P.budget;
-  const bool late = !P.mass && t >= P.window && C.n_scored[b] <= t - P.window;
-  const Plan p = plan_of(P, t, count, t >= P.window ? C.win_score[head * P.window + t % P.window] : 0.f, late);
-  load_kept_form<T, D, PK>(kw + (int64_t)p.slot * D, x_out);
-  load_kept_form<T, D, PK>(vw + (int64_t)p.slot * D, v_out);
 
   // the share's entry that goes first, and whether it is left out of the stream
   Entry low = {~0ull, -1};
@@ -642,8 +730,8 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
     };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
-      if (key0 + i * kStepThreads < key1) look(key_ahead[i], pos_ahead[i], key0 + i * kStepThreads);
-    for (int r = key0 + kAhead * kStepThreads; r < key1; r += kStepThreads) look(C.ret_score[head * P.budget + r], C.ret_pos[head * P.budget + r], r);
+      if (key0 + i * NT < key1) look(key_ahead[i], pos_ahead[i], key0 + i * NT);
+    for (int r = key0 + kAhead * NT; r < key1; r += NT) look(C.ret_score[head * P.budget + r], C.ret_pos[head * P.budget + r], r);
     low = first_of_wave(low);
     if (lane == 0) red_e[wave] = low;
     __syncthreads();
@@ -654,42 +742,27 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
   }
   low.slot = __builtin_amdgcn_readfirstlane(low.slot);
   int dst = -1;
-  if constexpr (MODE == kWhole) {
+  if constexpr (WHOLE) {
     dst = target_of(P, p, low);
     if (dst != low.slot) low.slot = -1;          // it stays: nothing is left out
   }
-  // scores of the incoming and of the leaving token; the leaving one's values as they would be kept
-  for (int i = wave; i < 2 * G; i += W) {
-    const int g = i >> 1, x = i & 1;
-    float part = 0.f;
-#pragma unroll
-    for (int s = 0; s < D / 64; ++s) part = fmaf(to_f32(q[((int64_t)b * P.Hq + h * G + g) * D + lane + 64 * s]), x ? x_out[s] : x_in[s], part);
-    part = wave_sum(part);
-    if (lane == 0) xs[x * G + g] = part * P.scale2;
-  }
-  if (wave == W - 1)
-#pragma unroll
-    for (int s = 0; s < D / 64; ++s) ve_lds[lane + 64 * s] = v_out[s];
-
   const int live_ring = t < P.window ? t : P.window;
   const int ring_end = sh.ring1 < (live_ring + 31) / 32 ? sh.ring1 : (live_ring + 31) / 32;
   const int kept_end = sh.kept1 < (count + 31) / 32 ? sh.kept1 : (count + 31) / 32;
   const int at_kept = 32 * ((P.window + 31) / 32);
-  const int col = Running<T, D, GT>::kTermColumns ? c & 7 : c;
-  const bool second = Running<T, D, GT>::kTermColumns && c >= 8;
   Running<T, D, GT> run;
-  for (int g0 = 0; g0 < G; g0 += GT) {
+  T q_ahead[2][D / 64];
+  FirstRows first;
+  for (int g0 = 0;;) {
     run.reset();
     const bool mine = g0 + col < G;
-    const T* qr = q + ((int64_t)b * P.Hq + h * G + (mine ? g0 + col : 0)) * D;
+    const T* qr = query_row(g0);
     const bool writes = P.mass && mine && !second;
     float* my_scores = rest + (int64_t)(g0 + col) * P.L.slots + 8 * kg;                               // in LDS
     const uint32_t my_offset = writes ? (uint32_t)(((g0 + col) * P.L.slots + 8 * kg) * 4) : 1u << 31;      // or in the workspace
-    Q qf[kQ];
-    // scores of a block -> log2 units, kept for the weights, then masked; special: a row of it that does not count (or none), n_live rows do
+    float q_reg[sizeof(T) == 4 ? kQ : 1];      // fp32
+    // scores of a block: kept for the weights, then masked; special: a row of it that does not count (or none), n_live rows do
     auto finish_scores = [&](float (&x)[8], int n_live, int special, int at, bool kept, bool partial) {
-#pragma unroll
-      for (int u = 0; u < 8; ++u) x[u] *= P.scale2;
       const f32x4 lo = {x[0], x[1], x[2], x[3]}, hi = {x[4], x[5], x[6], x[7]};
       if (P.scores_in_lds) {
         if (writes) {
@@ -697,10 +770,9 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
           *reinterpret_cast<f32x4*>(my_scores + at + 4) = hi;
         }
       } else if (P.mass) {
-        constexpr int kFlags = MODE == kLastShare ? kPastL2 : 0;     // another workgroup of this launch may read them
         const auto to = bytes_at(scores, (uint32_t)(P.L.scores() * sizeof(float)));
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, lo), to, my_offset + 4u * (uint32_t)at, 0, kFlags);
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, hi), to, my_offset + 4u * (uint32_t)at + 16u, 0, kFlags);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, lo), to, my_offset + 4u * (uint32_t)at, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, hi), to, my_offset + 4u * (uint32_t)at + 16u, 0, 0);
       }
       if (partial) {
         int r0 = 8 * kg;
@@ -721,40 +793,46 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
       for (int u = 0; u < 8; ++u) d |= (uint32_t)(r0 + u >= n_live || r0 + u == special) << u;
       return d;
     };
+    auto load_queries = [&](auto rows) {       // fp32
+      using RT = decltype(rows);
+      constexpr int E = std::is_same<RT, S>::value ? 4 : 8;
+#pragma unroll
+      for (int i = 0; i < kQ; ++i) q_reg[i] = mine ? qr[RT::k_channel(i / E, kg, i % E)] : 0.f;
+    };
+    auto scores_of = [&](const auto& rows, int set, float (&x)[8]) {
+      if constexpr (sizeof(T) == 4) {
+        score_rows<D>(rows, q_reg, x);
+      } else {
+        int at = set * kQ * kWave + lane;
+        asm volatile("" : "+v"(at));           // (read again for every block: not held in registers over the loop)
+        score_rows<D>(rows, q_lds + at, x);
+      }
+    };
     // blocks blk, blk + W, .. < end of rows whose first block is requested; next_k / next_v request another one
     auto walk = [&](auto& rows, int blk, int end, int live, int special_row, int at0, bool kept, auto&& next_k, auto&& next_v) {
       for (; blk < end; blk += W) {
         const int n_live = live - 32 * blk < 32 ? live - 32 * blk : 32, special = special_row - 32 * blk;
         const bool partial = n_live < 32 || (special >= 0 && special < 32);
         float x[8];
-        score_rows<D>(rows, qf, x);
+        scores_of(rows, 0, x);
         next_k(blk + W, blk + W < end);
         if (partial) rows.clear(dead_rows(n_live, special));
         finish_scores(x, n_live, special, at0 + 32 * blk, kept, partial);
-        run.add(rows, x, second);
+        run.add(rows, x, P.scale2, second);
         next_v(blk + W, blk + W < end);
       }
     };
-    auto load_queries = [&](auto rows) {
-      using RT = decltype(rows);
-#pragma unroll
-      for (int i = 0; i < kQ; ++i) {
-        if constexpr (sizeof(T) == 4) {
-          constexpr int E = std::is_same<RT, S>::value ? 4 : 8;
-          qf[i] = mine ? qr[RT::k_channel(i / E, kg, i % E)] : 0.f;
-        } else {
-          u32x4 x = *reinterpret_cast<const u32x4*>(qr + RT::k_channel(i, kg, 0));
-          if (!mine) x = u32x4{0u, 0u, 0u, 0u};
-          qf[i] = __builtin_bit_cast(bf16x8, x);
-        }
-      }
-    };
-    load_queries(S{});
-    if (g0 > 0) {
-      load_ring_k(first_ring, first_ring < ring_end);
-      load_ring_v(first_ring, first_ring < ring_end);
-    }
+    if constexpr (sizeof(T) == 4) load_queries(S{});
+    put_queries(g0);
+    __syncthreads();
     walk(R, first_ring, ring_end, live_ring, p.leaving >= 0 ? p.slot : -1, 0, false, load_ring_k, load_ring_v);
+    if (g0 == 0)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int g = wave + i * W < 2 * G ? (wave + i * W) >> 1 : 0;
+#pragma unroll
+        for (int s = 0; s < D / 64; ++s) q_ahead[i][s] = q[((int64_t)b * P.Hq + h * G + g) * D + lane + 64 * s];
+      }
     if constexpr (!PK) {
       auto load_k = [&](int blk, bool there) { R.load_k(kr + (int64_t)32 * blk * D, there ? P.budget - 32 * blk : 0); };
       auto load_v = [&](int blk, bool there) { R.load_v(vr + (int64_t)32 * blk * D, there ? P.budget - 32 * blk : 0); };
@@ -762,8 +840,8 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
       load_v(first_kept, first_kept < kept_end);
       walk(R, first_kept, kept_end, count, low.slot, at_kept, true, load_k, load_v);
     } else {
-      if (g0 > 0) request_packed();
-      load_queries(PackedRows<D>{});
+      if constexpr (D == 128) request_packed();
+      if constexpr (sizeof(T) == 4) load_queries(PackedRows<D>{});
       for (int blk0 = first_kept; blk0 < kept_end; blk0 += kDepth * W) {
 #pragma unroll
         for (int i = 0; i < kDepth; ++i) {
@@ -772,37 +850,62 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
             const int n_live = count - 32 * blk < 32 ? count - 32 * blk : 32, special = low.slot - 32 * blk;
             const bool partial = n_live < 32 || (special >= 0 && special < 32);
             float x[8];
-            score_rows<D>(K[i], qf, x);
+            scores_of(K[i], 1, x);
             if (partial) K[i].clear(dead_rows(n_live, special));
             finish_scores(x, n_live, special, at_kept + 32 * blk, true, partial);
-            run.add(K[i], x, second);
+            run.add(K[i], x, P.scale2, second);
           }
           K[i].load(blocks + (int64_t)(blk + kDepth * W) * PackGeo<D>::kBlock, blk + kDepth * W < kept_end);
         }
       }
     }
+    if (g0 == 0) {
+      wait_loads();
+      __syncthreads();
+      if constexpr (WHOLE) request_keys(C, P, head, sh, first);
+      // scores of the incoming and of the leaving token; the leaving one's values as they would be kept
+      float x_in[D / 64], x_out[D / 64];
+      load_kept_form<T, D, false>(rows_lds[0], x_in);
+      load_kept_form<T, D, PK>(rows_lds[1], x_out);
+      for (int i = wave; i < 2 * G; i += W) {
+        const int g = i >> 1, x = i & 1;
+        float part = 0.f;
+#pragma unroll
+        for (int s = 0; s < D / 64; ++s)
+          part = fmaf(to_f32(i < 2 * W ? q_ahead[i / W][s] : q[((int64_t)b * P.Hq + h * G + g) * D + lane + 64 * s]), x ? x_out[s] : x_in[s], part);
+        part = wave_sum(part);
+        if (lane == 0) xs[x * G + g] = part;
+      }
+      if (wave == W - 1) {
+        float v_out[D / 64];
+        load_kept_form<T, D, PK>(rows_lds[2], v_out);
+#pragma unroll
+        for (int s = 0; s < D / 64; ++s) ve_lds[lane + 64 * s] = v_out[s];
+      }
+    }
     // merge of the waves
     run.l = column_sum(run.l);
-    if (kg == 0) { red_m[wave][c] = run.m; red_l[wave][c] = run.l; }
+    if (kg == 0) { red_m[wave][c] = run.m * P.scale2; red_l[wave][c] = run.l; }
 #pragma unroll
     for (int x = 0; x < D / 16; ++x)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         float o = run.o[x][r];
-        if constexpr (Running<T, D, GT>::kTermColumns) o += __shfl_xor(o, 8, kWave);
+        if constexpr (Running<T, D, GT>::kTermColumns)          // the other term's column: eight lanes on, in the row of 16
+          o += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(o), 0x128, 0xf, 0xf, false));
         if (mine && !second) red_o[(wave * heads_at_once + col) * kRow + (D / 16) * (4 * kg + r) + x] = o;      // output tile x, row 4 kg + r
       }
     __syncthreads();
     const int heads = G - g0 < GT ? G - g0 : GT;
-    for (int i = tid; i < heads * D; i += kStepThreads) {
+    for (int i = tid; i < heads * D; i += NT) {
       const int gl = i / D, d = i - gl * D, g = g0 + gl;
       float M = -INFINITY, L = 0.f, A = 0.f;
 #pragma unroll
       for (int w = 0; w < W; ++w) M = fmaxf(M, red_m[w][gl]);
-      constexpr bool whole = MODE == kWhole;
+      constexpr bool whole = WHOLE;
       if (whole) {
-        M = fmaxf(M, xs[g]);
-        if (dst >= 0) M = fmaxf(M, xs[G + g]);
+        M = fmaxf(M, xs[g] * P.scale2);
+        if (dst >= 0) M = fmaxf(M, xs[G + g] * P.scale2);
       }
       const float ref = M == -INFINITY ? 0.f : M;
 #pragma unroll
@@ -812,7 +915,7 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
         A = fmaf(red_o[(w * heads_at_once + gl) * kRow + d], f, A);
       }
       if (whole) {
-        const float w_t = exp2_hw(xs[g] - ref), w_e = dst >= 0 ? exp2_hw(xs[G + g] - ref) : 0.f;
+        const float w_t = exp2_hw(fmaf(xs[g], P.scale2, -ref)), w_e = dst >= 0 ? exp2_hw(fmaf(xs[G + g], P.scale2, -ref)) : 0.f;
         L += w_t + w_e;
         A = fmaf(w_t, to_f32(v_new[head * D + d]), A);
         if (dst >= 0) A = fmaf(w_e, ve_lds[d], A);
@@ -820,15 +923,21 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
         out[((int64_t)b * P.Hq + h * G + g) * D + d] = from_f32<T>(late ? __builtin_nanf("") : A / L);
       } else {
         float* r = rec + 4 + G + D + (size_t)g * (D + 2);
-        if (d == 0) { give(r, M); give(r + 1, L); }
-        give(r + 2 + d, A);
+        if (d == 0) { r[0] = M; r[1] = L; }
+        r[2 + d] = A;
       }
     }
     __syncthreads();
+    g0 += GT;
+    if (g0 >= G) break;
+    request_queries(g0);
+    load_ring_k(first_ring, first_ring < ring_end);          // (here: requested rows are not held through the loops above)
+    load_ring_v(first_ring, first_ring < ring_end);
+    if constexpr (PK && D == 64) request_packed();
   }
 
-  if constexpr (MODE == kWhole) {
-    grow_keys(C, P, p, head, sh, dst, xs, top, inv, [&](int g, int at) {
+  if constexpr (WHOLE) {
+    grow_keys<NT>(C, P, p, head, sh, dst, xs, top, inv, first, false, [&](int g, int at) {
       return *reinterpret_cast<const f32x4*>(P.scores_in_lds ? rest + g * P.L.slots + at : scores + (int64_t)g * P.L.slots + at);
     });
   } else {
@@ -843,18 +952,17 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
           v = to_f32(vr[(int64_t)low.slot * D + tid]);
         }
       }
-      give(rec + 4 + G + tid, v);
+      rec[4 + G + tid] = v;
     }
-    for (int g = tid; g < G; g += kStepThreads) give(rec + 4 + g, low.slot >= 0 ? low_x[g] : -INFINITY);
+    for (int g = tid; g < G; g += NT) rec[4 + g] = low.slot >= 0 ? low_x[g] : -INFINITY;
     if (tid == 0) {
-      give(rec, __uint_as_float((uint32_t)(low.order >> 32)));
-      give(rec + 1, __uint_as_float((uint32_t)low.order));
-      give(rec + 2, __int_as_float(low.slot));
+      rec[0] = __uint_as_float((uint32_t)(low.order >> 32));
+      rec[1] = __uint_as_float((uint32_t)low.order);
+      rec[2] = __int_as_float(low.slot);
     }
-    if constexpr (MODE == kSecondLaunch) {
-      if (split != 0) return;
+    if (split == 0) {
       float* plan = P.plan + head * P.L.plan();
-      for (int g = tid; g < 2 * G; g += kStepThreads) plan[4 + g] = xs[g];
+      for (int g = tid; g < 2 * G; g += NT) plan[4 + g] = xs[g];
       if (tid < D) plan[4 + 2 * G + tid] = ve_lds[tid];
       if (tid == 0) {
         plan[0] = __int_as_float(t);
@@ -862,34 +970,14 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
         plan[2] = p.z_e;
         plan[3] = __int_as_float(late);
       }
-      return;
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // what this thread gave is there
-    __syncthreads();
-    if (tid == 0) last_lds = (atomicAdd(reinterpret_cast<unsigned*>(C.ret_count + head), 1u << 16) >> 16 & 255u) + 1u == (unsigned)n;
-    __syncthreads();
-    if (!last_lds) return;
-    const float* all = P.shares + head * n * P.L.share();
-    float* fac = rest;
-    float* stay = fac + G * n;
-    dst = join_shares<true, D>(P, p, all, xs, fac, stay, top, inv);
-    __syncthreads();
-    for (int i = tid; i < G * D; i += kStepThreads) {
-      const int g = i / D, d = i - g * D;
-      const float y = joined_output<true, T, D>(P, all, g, d, dst, xs, to_f32(v_new[head * D + d]), ve_lds[d], fac, stay, top, inv);
-      out[((int64_t)b * P.Hq + h * G + g) * D + d] = from_f32<T>(late ? __builtin_nanf("") : y);
-    }
-    const auto from = bytes_at(scores, (uint32_t)(P.L.scores() * sizeof(float)));
-    grow_keys(C, P, p, head, Share{0, (P.window + 31) / 32, 0, (P.budget + 31) / 32}, dst, xs, top, inv, [&](int g, int at) {
-      return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, (uint32_t)(g * P.L.slots + at) * 4u, 0, kPastL2));
-    });
+    return;
   }
   // every row has been read
   if (tid < D) move_rows<T, D, PK>(C, P, p, head, dst, k_new[head * D + tid], v_new[head * D + tid]);
   if (tid == 0) {
-    const unsigned delta = (dst >= 0 && dst == count ? 1u : 0u) - (n > 1 ? (unsigned)n << 16 : 0u);
     unsigned* words = reinterpret_cast<unsigned*>(C.ret_count + (int64_t)b * P.Hkv);
-    if (delta != 0u) atomicAdd(words + h, delta);
+    if (dst >= 0 && dst == count) atomicAdd(words + h, 1u);
     const bool last_head = P.Hkv == 1 || (atomicAdd(words, 1u << 24) >> 24) + 1u == (unsigned)P.Hkv;
     if (last_head) {
       if (P.Hkv > 1) atomicSub(words, (unsigned)P.Hkv << 24);
@@ -917,16 +1005,26 @@ kept_finish_kernel(CacheDev C, KeptParams P, const T* __restrict__ k_new, const 
   float* inv = top + G;
   const Plan p = plan_of(P, __float_as_int(plan[0]), __float_as_int(plan[1]), plan[2], __float_as_int(plan[3]) != 0);
   const float* xs = plan + 4;
-  const int dst = join_shares<false, D>(P, p, rec, xs, fac, stay, top, inv);
+  const Share sh = share_of(P, split);
+  const auto from = bytes_at(scores, (uint32_t)(P.L.scores() * sizeof(float)));
+  auto score4 = [&](int g, int at) {
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, (uint32_t)(g * P.L.slots + at) * 4u, 0, 0));
+  };
+  const int items = G * D, i0 = (int)((int64_t)items * split / n) + tid, i1 = (int)((int64_t)items * (split + 1) / n);
+  FirstShares F;
+  FirstRows first;
+  take_shares<D>(P, rec, i0 < items ? i0 / D : 0, i0 % D, 0, F);
+  request_keys(C, P, head, sh, first);
+  request_scores(P, sh, first, score4);
+  const int dst = join_shares<D>(P, p, rec, xs, fac, stay, top, inv);
   __syncthreads();
-  const int items = G * D, i0 = (int)((int64_t)items * split / n), i1 = (int)((int64_t)items * (split + 1) / n);
-  for (int i = i0 + tid; i < i1; i += kStepThreads) {
+  for (int i = i0; i < i1; i += kStepThreads) {
     const int g = i / D, d = i - g * D;
-    const float y = joined_output<false, T, D>(P, rec, g, d, dst, xs, to_f32(v_new[head * D + d]), plan[4 + 2 * G + d], fac, stay, top, inv);
+    if (i != i0) take_shares<D>(P, rec, g, d, 0, F);
+    const float y = joined_output<D>(P, rec, g, d, dst, xs, to_f32(v_new[head * D + d]), plan[4 + 2 * G + d], fac, stay, top, inv, F);
     out[((int64_t)b * P.Hq + h * G + g) * D + d] = from_f32<T>(p.late ? __builtin_nanf("") : y);
   }
-  grow_keys(C, P, p, head, share_of(P, split), dst, xs, top, inv,
-            [&](int g, int at) { return *reinterpret_cast<const f32x4*>(scores + (int64_t)g * P.L.slots + at); });
+  grow_keys<kStepThreads>(C, P, p, head, sh, dst, xs, top, inv, first, true, score4);
   if (split != 0) return;
   if (tid < D) move_rows<T, D, PK>(C, P, p, head, dst, k_new[head * D + tid], v_new[head * D + tid]);
   if (tid == 0) {
@@ -939,7 +1037,7 @@ kept_finish_kernel(CacheDev C, KeptParams P, const T* __restrict__ k_new, const 
 }
 
 template <typename T, int D>
-hipError_t kept_run(const ltea_cfg& cfg, const KeptInputs& in, const ltea_cache& c, int n_seqs, int nsplit, void* workspace,
+hipError_t kept_run(const ltea_cfg& cfg, const KeptInputs& in, const ltea_cache& c, int n_seqs, KeptSplit split, void* workspace,
                     hipStream_t stream) {
   CacheDev C{c.k_win, c.v_win, c.win_score, c.k_ret, c.v_ret, c.ret_score, c.ret_pos, c.ret_count, c.n_seen, c.n_scored};
   KeptParams P;
@@ -949,41 +1047,48 @@ hipError_t kept_run(const ltea_cfg& cfg, const KeptInputs& in, const ltea_cache&
   P.scale2 = (cfg.softmax_scale > 0.f ? cfg.softmax_scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
   P.packed = static_cast<const uint8_t*>(in.packed);
   P.status = in.status;
-  const int G = cfg.Hq / cfg.Hkv;
+  const int G = cfg.Hq / cfg.Hkv, nsplit = split.shares;
   P.L = KeptLayout{G, D, nsplit, 32 * (kept_blocks_of(cfg.window) + kept_blocks_of(cfg.budget))};
-  // counts fit ret_count's upper bits, and what is left to the last share to arrive is not more than a second launch costs
-  P.fused = cfg.budget > 0 && cfg.budget < (1 << 16) && cfg.Hkv <= 255 && (nsplit == 1 || !in.mass || P.L.scores() <= kKeptLastShare);
-  P.count_mask = P.fused ? 0xFFFFu : 0xFFFFFFFFu;
-  P.scores_in_lds = P.fused && nsplit == 1 && P.L.scores() * sizeof(float) <= kKeptScoresLds;
+  // a whole head's workgroup finishes it where its count fits ret_count's upper bits
+  const bool whole = nsplit == 1 && cfg.budget > 0 && cfg.budget < (1 << 16) && cfg.Hkv <= 255;
+  P.count_mask = whole ? 0xFFFFu : 0xFFFFFFFFu;
   const int64_t heads = (int64_t)n_seqs * cfg.Hkv;
   P.plan = static_cast<float*>(workspace);
   P.shares = P.plan + (P.L.plan() * heads + 63) / 64 * 64;
   P.scores = P.shares + (P.L.share() * heads * nsplit + 63) / 64 * 64;
   const dim3 grid((unsigned)(heads * nsplit));
-  auto go_mode = [&](auto pk, auto gt, auto mode) {
-    constexpr bool PK = decltype(pk)::value;
-    constexpr int GT = decltype(gt)::value;
-    const size_t rest = P.scores_in_lds ? (in.mass ? P.L.scores() : 0) : P.fused && nsplit > 1 ? 2 * (size_t)G * nsplit : 0;
-    const size_t bytes = ((size_t)kStepWaves * (G < GT ? G : GT) * (D + 4) + 6 * (size_t)G + 4 + rest) * sizeof(float);
-    hipLaunchKernelGGL((kept_step_kernel<T, D, PK, GT, decltype(mode)::value>), grid, dim3(kStepThreads), bytes, stream, C, P, static_cast<const T*>(in.q),
-                       static_cast<const T*>(in.k), static_cast<const T*>(in.v), static_cast<T*>(in.out));
+  auto launch = [&](auto pk, auto gt, auto finishes, auto waves) {
+    constexpr bool PK = decltype(pk)::value, WHOLE = decltype(finishes)::value;
+    constexpr int GT = decltype(gt)::value, W = decltype(waves)::value;
+    size_t bytes = ((size_t)W * (G < GT ? G : GT) * (D + 4) + 6 * (size_t)G + 4) * sizeof(float);
+    const size_t rest = in.mass ? P.L.scores() * sizeof(float) : 0;
+    P.scores_in_lds = WHOLE && rest <= kKeptScoresLds && bytes + rest <= kKeptLds;
+    if (P.scores_in_lds) bytes += rest;
+    hipLaunchKernelGGL((kept_step_kernel<T, D, PK, GT, WHOLE, W>), grid, dim3(W * kWave), bytes, stream, C, P,
+                       static_cast<const T*>(in.q), static_cast<const T*>(in.k), static_cast<const T*>(in.v), static_cast<T*>(in.out));
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || P.fused) return e;
+    if (e != hipSuccess || WHOLE) return e;
     hipLaunchKernelGGL((kept_finish_kernel<T, D, PK>), grid, dim3(kStepThreads), (size_t)(2 * G * nsplit + 2 * G) * sizeof(float),
                        stream, C, P, static_cast<const T*>(in.k), static_cast<const T*>(in.v), static_cast<T*>(in.out));
     return hipGetLastError();
   };
+  using std::integral_constant;
+  using std::true_type;
   auto go = [&](auto pk, auto gt) {
-    if (!P.fused) return go_mode(pk, gt, std::integral_constant<int, kSecondLaunch>{});
-    return nsplit == 1 ? go_mode(pk, gt, std::integral_constant<int, kWhole>{}) : go_mode(pk, gt, std::integral_constant<int, kLastShare>{});
+    const integral_constant<int, kStepWaves> four;
+    if (!whole) return launch(pk, gt, std::false_type{}, four);
+    if constexpr (decltype(gt)::value * D <= 1024) {          // (the outputs of eight waves: 34 KB of LDS)
+      if (split.waves == 8) return launch(pk, gt, true_type{}, integral_constant<int, 8>{});
+    }
+    return launch(pk, gt, true_type{}, four);
   };
   auto by_heads = [&](auto pk) {
     if constexpr (sizeof(T) == 2) {
-      if (G <= 8) return go(pk, std::integral_constant<int, 8>{});
+      if (G <= 8) return go(pk, integral_constant<int, 8>{});
     }
-    return go(pk, std::integral_constant<int, 16>{});
+    return go(pk, integral_constant<int, 16>{});
   };
-  return in.packed != nullptr ? by_heads(std::integral_constant<bool, true>{}) : by_heads(std::integral_constant<bool, false>{});
+  return in.packed != nullptr ? by_heads(true_type{}) : by_heads(std::false_type{});
 }
 
 }  // namespace

@@ -3,6 +3,6 @@
 
 namespace ltea {
 
-LTEA_KEPT_RUN(kept_run_bf16_128) { return kept_run<bf16_t, 128>(cfg, in, c, n_seqs, nsplit, workspace, stream); }
+LTEA_KEPT_RUN(kept_run_bf16_128) { return kept_run<bf16_t, 128>(cfg, in, c, n_seqs, split, workspace, stream); }
 
 }  // namespace ltea

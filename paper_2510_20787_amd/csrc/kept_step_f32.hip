@@ -3,7 +3,7 @@
 
 namespace ltea {
 
-LTEA_KEPT_RUN(kept_run_f32_64) { return kept_run<float, 64>(cfg, in, c, n_seqs, nsplit, workspace, stream); }
-LTEA_KEPT_RUN(kept_run_f32_128) { return kept_run<float, 128>(cfg, in, c, n_seqs, nsplit, workspace, stream); }
+LTEA_KEPT_RUN(kept_run_f32_64) { return kept_run<float, 64>(cfg, in, c, n_seqs, split, workspace, stream); }
+LTEA_KEPT_RUN(kept_run_f32_128) { return kept_run<float, 128>(cfg, in, c, n_seqs, split, workspace, stream); }
 
 }  // namespace ltea
