@@ -17,7 +17,10 @@
 namespace ltea {
 namespace {
 
-constexpr int kThreads = 256, kTileRows = 64;
+constexpr int kThreads = 256, kStepRows = 64;
+// Rows of a tile of queries: steps of 64, one barrier.  bf16: two steps (4 x 4096 tokens, 32/8 heads, D = 64: 227 us, with one 267;
+// 32768 tokens, 32 heads, D = 128: 4316 and 4363); fp32 fills the LDS with one.
+template <typename T, int D> constexpr int kRows = sizeof(T) == 2 ? 128 : 64;
 // Blocks of 32 keys per wave, keys per workgroup
 template <typename T, int D> constexpr int kKeyBlocks = sizeof(T) == 4 ? 1 : 2;
 template <typename T, int D> constexpr int kTileKeys = 4 * 32 * kKeyBlocks<T, D>;
@@ -37,7 +40,7 @@ __device__ __forceinline__ void queries_of(const MassParams& P, int part, int n,
   const int first = P.last > 0 && n > P.last ? n - P.last : 0;
   const int64_t from = first + (int64_t)part * P.part_rows, reach = (int64_t)hi - 1 + P.window;
   const int64_t to = from + P.part_rows < reach ? from + P.part_rows : reach;
-  q0 = (int)(from < lo ? lo / kTileRows * kTileRows > from ? lo / kTileRows * kTileRows : from : from < n ? from : n);
+  q0 = (int)(from < lo ? lo / kStepRows * kStepRows > from ? lo / kStepRows * kStepRows : from : from < n ? from : n);
   q1 = (int)(to < n ? to : n);
 }
 
@@ -46,11 +49,12 @@ __global__ void __launch_bounds__(kThreads, 2)
 attention_mass_kernel(const T* __restrict__ q, int64_t q_st, int64_t q_sh, const T* __restrict__ k, int64_t k_st, int64_t k_sh,
                       const int32_t* __restrict__ cu, const float* __restrict__ lse, MassParams P, float* __restrict__ sums) {
   constexpr int KB = kKeyBlocks<T, D>, kKeys = kTileKeys<T, D>;
+  constexpr int kTileRows = kRows<T, D>, kSteps = kTileRows / kStepRows;
   constexpr int kRow = D * (int)sizeof(T), PPR = kRow / 16, KP = PPR / 2;       // 16-byte pieces of a row, and per lane
   constexpr int kLoads = kTileRows * PPR / kThreads;
   __shared__ __align__(1024) uint8_t tile[2][kTileRows * kRow];
   __shared__ float tile_lse[2][kTileRows];
-  __shared__ int tile_whole[2];
+  __shared__ int tile_whole[2][kSteps];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), c = lane & 31, hb = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   // An XCD takes whole (part, KV head) units: the key tiles that read the same queries run side by side on its L2.  Late parts, which
@@ -106,16 +110,16 @@ attention_mass_kernel(const T* __restrict__ q, int64_t q_st, int64_t q_sh, const
     const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, (uint32_t)(rows - 1) * row_bytes + (uint32_t)kRow, 0x00020000);
 #pragma unroll
     for (int x = 0; x < kLoads; ++x) held[x] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, from[x], 0, 0);
-    if (wave == 0) held_lse = lse[(int64_t)(h * G + g) * P.total + lo + (r0 + lane < n ? r0 + lane : n - 1)];
+    if (wave < kSteps) held_lse = lse[(int64_t)(h * G + g) * P.total + lo + (r0 + tid < n ? r0 + tid : n - 1)];
   };
   auto put = [&](int buf, int r0) {
 #pragma unroll
     for (int x = 0; x < kLoads; ++x) *reinterpret_cast<u32x4*>(&tile[buf][into[x]]) = held[x];
-    if (wave == 0) {
-      const bool counts = r0 + lane < q1 && fabsf(held_lse) < INFINITY;     // a query whose lse is not finite counts nothing
-      tile_lse[buf][lane] = counts ? held_lse * 1.4426950408889634f : INFINITY;
+    if (wave < kSteps) {
+      const bool counts = r0 + tid < q1 && fabsf(held_lse) < INFINITY;     // a query whose lse is not finite counts nothing
+      tile_lse[buf][tid] = counts ? held_lse * 1.4426950408889634f : INFINITY;
       const bool all = __builtin_amdgcn_ballot_w64(counts) == ~0ull;
-      if (lane == 0) tile_whole[buf] = all;
+      if (lane == 0) tile_whole[buf][wave] = all;
     }
   };
   // The block whose scores are there but whose exponentials are not taken yet: they go between the next block's matrix instructions.
@@ -148,62 +152,66 @@ attention_mass_kernel(const T* __restrict__ q, int64_t q_st, int64_t q_sh, const
     const bool wraps = r0 + kTileRows >= q1;
     const int g_next = wraps ? g + 1 : g, r_next = wraps ? q0 : r0 + kTileRows;
     if (g_next < G) request(g_next, r_next);
-    // every query of the tile counts and sees every key of the wave
-    const bool plain = tile_whole[buf] && r0 >= my0 + 32 * KB - 1 && r0 + kTileRows - 1 - my0 < P.window && my0 < n;
-    if (plain) {
-      u32x4 qf[KP];
-      float l2 = 0.f, l_old = pending;
-#pragma unroll
-      for (int st = 0; st < 2 * KB; ++st) {
-        const int half = st / KB, x = st % KB, now = st & 1, old = now ^ 1, xo = (st + KB * 2 - 1) % KB;
-        if (x == 0) load_q(buf, half, qf, l2);
-        s[now] = zero;
-        // the first matrix instruction goes before the exponentials that wait for the last one of the block before
-#pragma unroll
-        for (int p = 0; p < KP; ++p) {
-          s[now] = mma(kf[x][p], qf[p], s[now]);
-          if (p > 0)
-#pragma unroll
-            for (int y = 16 * (p - 1) / (KP - 1); y < 16 * p / (KP - 1); ++y)
-              sum[xo][y] += __builtin_amdgcn_exp2f(fmaf(s[old][y], P.scale2, -l_old));
-          if constexpr (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
-        }
-        l_old = l2;
-      }
-      pending = l2;
-    }
-    if (!plain && my0 < n) {
-#pragma unroll
-      for (int y = 0; y < 16; ++y) {
-        sum[KB - 1][y] += __builtin_amdgcn_exp2f(fmaf(s[1][y], P.scale2, -pending));
-        s[1][y] = -INFINITY;
-      }
 #pragma unroll 1
-      for (int half = 0; half < 2; ++half) {
-        const int i0 = r0 + 32 * half, i_q = i0 + c;
-        // no query, all queries before the wave's keys, or all keys out of their windows
-        if (i0 >= q1 || i0 + 31 < my0 || i0 - (my0 + 32 * KB - 1) >= P.window) continue;
+    for (int step = 0; step < kSteps; ++step) {
+      // every query of the step counts and sees every key of the wave
+      const int r1 = r0 + kStepRows * step;
+      const bool plain = tile_whole[buf][step] && r1 >= my0 + 32 * KB - 1 && r1 + kStepRows - 1 - my0 < P.window && my0 < n;
+      if (plain) {
         u32x4 qf[KP];
-        float l2;
-        load_q(buf, half, qf, l2);
-        if (!(l2 < INFINITY))
+        float l2 = 0.f, l_old = pending;
 #pragma unroll
-          for (int p = 0; p < KP; ++p) qf[p] = u32x4{0u, 0u, 0u, 0u};
+        for (int st = 0; st < 2 * KB; ++st) {
+          const int half = st / KB, x = st % KB, now = st & 1, old = now ^ 1, xo = (st + KB * 2 - 1) % KB;
+          if (x == 0) load_q(buf, 2 * step + half, qf, l2);
+          s[now] = zero;
+          // the first matrix instruction goes before the exponentials that wait for the last one of the block before
 #pragma unroll
-        for (int x = 0; x < KB; ++x) {
-          const int j0 = my0 + 32 * x;
-          f32x16 z = zero;
+          for (int p = 0; p < KP; ++p) {
+            s[now] = mma(kf[x][p], qf[p], s[now]);
+            if (p > 0)
 #pragma unroll
-          for (int p = 0; p < KP; ++p) z = mma(kf[x][p], qf[p], z);
+              for (int y = 16 * (p - 1) / (KP - 1); y < 16 * p / (KP - 1); ++y)
+                sum[xo][y] += __builtin_amdgcn_exp2f(fmaf(s[old][y], P.scale2, -l_old));
+            if constexpr (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
+          }
+          l_old = l2;
+        }
+        pending = l2;
+      }
+      if (!plain && my0 < n) {
 #pragma unroll
-          for (int y = 0; y < 16; ++y) {
-            const int ago = i_q - (j0 + 8 * (y / 4) + 4 * hb + y % 4);
-            const float e = __builtin_amdgcn_exp2f(fmaf(z[y], P.scale2, -l2));
-            sum[x][y] += ago >= 0 && ago < P.window ? e : 0.f;
+        for (int y = 0; y < 16; ++y) {
+          sum[KB - 1][y] += __builtin_amdgcn_exp2f(fmaf(s[1][y], P.scale2, -pending));
+          s[1][y] = -INFINITY;
+        }
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          const int i0 = r1 + 32 * half, i_q = i0 + c;
+          // no query, all queries before the wave's keys, or all keys out of their windows
+          if (i0 >= q1 || i0 + 31 < my0 || i0 - (my0 + 32 * KB - 1) >= P.window) continue;
+          u32x4 qf[KP];
+          float l2;
+          load_q(buf, 2 * step + half, qf, l2);
+          if (!(l2 < INFINITY))
+#pragma unroll
+            for (int p = 0; p < KP; ++p) qf[p] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+          for (int x = 0; x < KB; ++x) {
+            const int j0 = my0 + 32 * x;
+            f32x16 z = zero;
+#pragma unroll
+            for (int p = 0; p < KP; ++p) z = mma(kf[x][p], qf[p], z);
+#pragma unroll
+            for (int y = 0; y < 16; ++y) {
+              const int ago = i_q - (j0 + 8 * (y / 4) + 4 * hb + y % 4);
+              const float e = __builtin_amdgcn_exp2f(fmaf(z[y], P.scale2, -l2));
+              sum[x][y] += ago >= 0 && ago < P.window ? e : 0.f;
+            }
           }
         }
+        pending = 0.f;
       }
-      pending = 0.f;
     }
     if (g_next < G) put(buf ^ 1, r_next);
     __syncthreads();
@@ -212,16 +220,26 @@ attention_mass_kernel(const T* __restrict__ q, int64_t q_st, int64_t q_sh, const
   }
 #pragma unroll
   for (int y = 0; y < 16; ++y) sum[KB - 1][y] += __builtin_amdgcn_exp2f(fmaf(s[1][y], P.scale2, -pending));
+  // Sums over the 32 query columns, halving the sums that a lane holds at every step: lane c ends with the one of y = c / 2.
 #pragma unroll
-  for (int x = 0; x < KB; ++x)
+  for (int x = 0; x < KB; ++x) {
 #pragma unroll
-    for (int y = 0; y < 16; ++y) {
-      float v = sum[x][y];
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
-      const int j = my0 + 32 * x + 8 * (y / 4) + 4 * hb + y % 4;
-      if (c == 0 && j < n) to[j] = v;
+    for (int y = 0; y < 8; ++y) {
+      const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(sum[x][y]), __float_as_uint(sum[x][y + 8]), false, false);
+      sum[x][y] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
     }
+#pragma unroll
+    for (int w = 4; w > 0; w >>= 1)
+#pragma unroll
+      for (int y = 0; y < w; ++y) {
+        const bool upper = c & 2 * w;
+        const float keep = upper ? sum[x][y + w] : sum[x][y], give = upper ? sum[x][y] : sum[x][y + w];
+        sum[x][y] = keep + __shfl_xor(give, 2 * w, kWave);
+      }
+    const float v = sum[x][0] + __shfl_xor(sum[x][0], 1, kWave);
+    const int y = c >> 1, j = my0 + 32 * x + 8 * (y / 4) + 4 * hb + y % 4;
+    if ((c & 1) == 0 && j < n) to[j] = v;
+  }
 }
 
 __global__ void __launch_bounds__(kThreads)
@@ -242,7 +260,7 @@ Split split_of(const ltea_cfg& cfg, const SeqView& sv, int last) {
   const int64_t reach = last > 0 && last < sv.max_seqlen ? last : sv.max_seqlen;
   int64_t parts = (kFill + groups - 1) / groups;
   if (parts < (reach + 2047) / 2048) parts = (reach + 2047) / 2048;
-  int64_t rows = ((reach + parts - 1) / parts + kTileRows - 1) / kTileRows * kTileRows;
+  int64_t rows = ((reach + parts - 1) / parts + kStepRows - 1) / kStepRows * kStepRows;
   return Split{(int)((reach + rows - 1) / rows), (int)rows};
 }
 
@@ -260,7 +278,7 @@ size_t mass_workspace_most(const ltea_cfg& cfg, int64_t total, int32_t max_seqle
 
 // The grid and the offsets inside a tile of queries are 32-bit numbers.
 bool mass_supported(const ltea_cfg& cfg, const SeqView& sv, int64_t q_st, int last) {
-  if (q_st * (cfg.dtype == LTEA_F32 ? 4 : 2) * kTileRows >= (int64_t)1 << 31) return false;
+  if (q_st * (cfg.dtype == LTEA_F32 ? 4 : 2) * 128 >= (int64_t)1 << 31) return false;
   const int64_t keys = tile_keys(cfg);
   return sv.total_tokens == 0 || (sv.total_tokens / keys + sv.n_seqs) * ((int64_t)cfg.Hkv * split_of(cfg, sv, last).parts + 7) <= INT32_MAX;
 }
