@@ -69,4 +69,59 @@ __device__ __forceinline__ float code_value(uint32_t code, float scale) {
   return (code & 8u ? -a : a) * scale;
 }
 
+// The same by the chip's conversions, two values at a time: byte `byte` of codes.  2^E is given as group_scale() has it; they read its
+// exponent bits, and give NaN for 255.
+__device__ __forceinline__ uint32_t bf16_pair(uint32_t codes, float scale, int byte) {
+  bf16x2 r;
+  switch (byte) {          // an immediate of the instruction
+    case 0: r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0); break;
+    case 1: r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1); break;
+    case 2: r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2); break;
+    default: r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3); break;
+  }
+  return __builtin_bit_cast(uint32_t, r);
+}
+
+// The same as two fp32 values.
+__device__ __forceinline__ void f32_pair(uint32_t codes, float scale, int byte, float& a, float& b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  f32x2 r;
+  switch (byte) {
+    case 0: r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0); break;
+    case 1: r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1); break;
+    case 2: r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2); break;
+    default: r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3); break;
+  }
+  a = r[0];
+  b = r[1];
+}
+
+// Codes of two values into byte `byte` of codes; the quotient by 2^E rounded as value_code does.
+__device__ __forceinline__ uint32_t pair_codes(uint32_t codes, float a, float b, float scale, int byte) {
+  switch (byte) {
+    case 0: return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, a, b, scale, 0);
+    case 1: return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, a, b, scale, 1);
+    case 2: return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, a, b, scale, 2);
+    default: return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, a, b, scale, 3);
+  }
+}
+__device__ __forceinline__ uint32_t pair_codes(uint32_t codes, uint32_t two_bf16, float scale, int byte) {
+  const bf16x2 x = __builtin_bit_cast(bf16x2, two_bf16);
+  switch (byte) {
+    case 0: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, x, scale, 0);
+    case 1: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, x, scale, 1);
+    case 2: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, x, scale, 2);
+    default: return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, x, scale, 3);
+  }
+}
+
+// `bytes` bytes at p, the same in all lanes; what lies past them reads as zeros and is not written.
+__device__ __forceinline__ auto bytes_at(const void* p, uint32_t bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(p);        // (the compiler does not see that this is the same in all lanes)
+  void* same = reinterpret_cast<void*>((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) << 32 |
+                                       (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a));
+  return __builtin_amdgcn_make_buffer_rsrc(same, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+constexpr int kNonTemporal = 2;              // of buffer instructions
+
 }  // namespace ltea

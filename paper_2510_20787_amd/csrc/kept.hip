@@ -8,31 +8,71 @@ namespace {
 
 // ---- rows <-> 4 bits ------------------------------------------------------------------------------------------------------------
 // One workgroup per block of 32 rows of a head; a thread takes eight channels of a row at a time, four neighbouring threads a group.
-// Bound: HBM (D = 128, bf16: 512 bytes of row against 136).
+// Bound: HBM (D = 128, bf16: 512 bytes of row against 136), with everything a workgroup reads requested at once and the chip's
+// conversions (16 sequences x 8 heads x 8192 rows: 108 us there and 95 back; rounding by comparisons 193 there).
 constexpr int kPackThreads = 256;
 
-template <typename T> __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
-  if constexpr (sizeof(T) == 4) {
-    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+// Eight channels as the workgroup's memory holds them.
+template <typename T> struct Eight {
+  uint32_t w[2 * sizeof(T)];
+  template <typename R> __device__ __forceinline__ void load(const R& rsrc, uint32_t at) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
-  } else {
-    const u32x4 a = *reinterpret_cast<const u32x4*>(p);
+    for (int p = 0; p < (int)sizeof(T) / 2; ++p) {
+      const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at + 16 * p, 0, kNonTemporal);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(a[i] << 16); x[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u); }
+      for (int e = 0; e < 4; ++e) w[4 * p + e] = x[e];
+    }
   }
-}
-template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
-  if constexpr (sizeof(T) == 4) {
-    reinterpret_cast<f32x4*>(p)[0] = f32x4{x[0], x[1], x[2], x[3]};
-    reinterpret_cast<f32x4*>(p)[1] = f32x4{x[4], x[5], x[6], x[7]};
-  } else {
-    bf16x8 a;
+  template <typename R> __device__ __forceinline__ void store(const R& rsrc, uint32_t at) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) a[i] = (bf16_t)x[i];
-    *reinterpret_cast<bf16x8*>(p) = a;
+    for (int p = 0; p < (int)sizeof(T) / 2; ++p)
+      __builtin_amdgcn_raw_buffer_store_b128(u32x4{w[4 * p], w[4 * p + 1], w[4 * p + 2], w[4 * p + 3]}, rsrc, at + 16 * p, 0, kNonTemporal);
   }
-}
+  // bits of the largest magnitude as fp32
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t m = 0u;
+#pragma unroll
+    for (int e = 0; e < (int)(2 * sizeof(T)); ++e) {
+      if constexpr (sizeof(T) == 4) {
+        const uint32_t a = w[e] & 0x7FFFFFFFu;
+        m = a > m ? a : m;
+      } else {
+        const uint32_t a = w[e] << 16 & 0x7FFFFFFFu, b = w[e] & 0x7FFF0000u;
+        m = a > m ? a : m;
+        m = b > m ? b : m;
+      }
+    }
+    return m;
+  }
+  __device__ __forceinline__ uint32_t codes(float scale) const {
+    uint32_t c = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) c = pair_codes(c, __uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]), scale, i);
+      else c = pair_codes(c, w[i], scale, i);
+    }
+    return c;
+  }
+  __device__ __forceinline__ uint32_t signs() const {       // codes of zeros with the values' signs
+    uint32_t c = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c |= (sizeof(T) == 4 ? w[i % (2 * sizeof(T))] >> 31 : w[i / 2] >> (16 * (i & 1) + 15) & 1u) << (4 * i + 3);
+    return c;
+  }
+  __device__ __forceinline__ void set(uint32_t c, float scale) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        float a, b;
+        f32_pair(c, scale, i, a, b);
+        w[2 * i] = __float_as_uint(a);
+        w[2 * i + 1] = __float_as_uint(b);
+      } else {
+        w[i] = bf16_pair(c, scale, i);
+      }
+    }
+  }
+};
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kPackThreads)
@@ -43,39 +83,41 @@ kept_pack_kernel(const T* __restrict__ k_ret, const T* __restrict__ v_ret, const
   const int left = ret_count[head] - 32 * blk;
   if (left <= 0) return;
   uint8_t* out = packed + (head * n_blocks + blk) * (int64_t)PackGeo<D>::kBlock;
-  constexpr int kItems = 2 * 32 * D / 8;
+  constexpr int kEach = 32 * D / 8 / kPackThreads;          // items of K, and of V, per thread
+  static_assert(kEach * kPackThreads * 8 == 32 * D, "whole rounds");
+  const int64_t row0 = (head * budget + 32 * blk) * D;
+  const uint32_t bytes = (uint32_t)((left < 32 ? left : 32) * D * (int)sizeof(T));      // rows past them read as zeros
+  const auto rk = bytes_at(k_ret + row0, bytes), rv = bytes_at(v_ret + row0, bytes);
+  Eight<T> x[2][kEach];
 #pragma unroll
-  for (int i = threadIdx.x; i < kItems; i += kPackThreads) {
-    const int d = 8 * (i % (D / 8)), r = i / (D / 8) % 32;
-    const bool is_v = i >= kItems / 2;
-    if (r >= left) continue;                 // (whole groups of four threads)
-    float x[8];
-    load8((is_v ? v_ret : k_ret) + (head * budget + 32 * blk + r) * D + d, x);
-    uint32_t top = 0u;
+  for (int i = 0; i < kEach; ++i) x[0][i].load(rk, (uint32_t)(threadIdx.x + i * kPackThreads) * 8u * (uint32_t)sizeof(T));
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t a = __float_as_uint(x[e]) & 0x7FFFFFFFu;
-      top = a > top ? a : top;
+  for (int i = 0; i < kEach; ++i) x[1][i].load(rv, (uint32_t)(threadIdx.x + i * kPackThreads) * 8u * (uint32_t)sizeof(T));
+#pragma unroll
+  for (int is_v = 0; is_v < 2; ++is_v)
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int item = threadIdx.x + i * kPackThreads, d = 8 * (item % (D / 8)), r = item / (D / 8);
+      uint32_t top = x[is_v][i].top();
+      uint32_t other = __builtin_amdgcn_update_dpp(0, top, 0xB1, 0xf, 0xf, false);      // lane ^ 1
+      top = other > top ? other : top;
+      other = __builtin_amdgcn_update_dpp(0, top, 0x4E, 0xf, 0xf, false);               // lane ^ 2
+      top = other > top ? other : top;
+      const uint32_t ex = group_exponent(top);
+      uint32_t codes = x[is_v][i].codes(group_scale(ex));
+      if (top < 0x03800000u) codes = x[is_v][i].signs();
+      if (ex == 255u) codes = 0x77777777u;
+      if (r >= left) continue;
+      if (!is_v) {
+        *reinterpret_cast<uint32_t*>(out + k_code_at<D>(r, d)) = codes;
+      } else if constexpr (D == 128) {
+        *reinterpret_cast<uint32_t*>(out + v_code_at<D>(r, d)) = codes;
+      } else {
+        *reinterpret_cast<uint16_t*>(out + v_code_at<D>(r, d)) = (uint16_t)codes;
+        *reinterpret_cast<uint16_t*>(out + v_code_at<D>(r, d + 4)) = (uint16_t)(codes >> 16);
+      }
+      if (d % 32 == 0) out[is_v ? v_exp_at<D>(r, d / 32) : k_exp_at<D>(r, d / 32)] = (uint8_t)ex;
     }
-#pragma unroll
-    for (int off = 1; off <= 2; off <<= 1) {
-      const uint32_t y = (uint32_t)__shfl_xor((int)top, off, kWave);
-      top = y > top ? y : top;
-    }
-    const uint32_t ex = group_exponent(top);
-    uint32_t codes = 0u;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) codes |= value_code(__float_as_uint(x[e]), ex, top) << (4 * e);
-    if (!is_v) {
-      *reinterpret_cast<uint32_t*>(out + k_code_at<D>(r, d)) = codes;
-    } else if constexpr (D == 128) {
-      *reinterpret_cast<uint32_t*>(out + v_code_at<D>(r, d)) = codes;
-    } else {
-      *reinterpret_cast<uint16_t*>(out + v_code_at<D>(r, d)) = (uint16_t)codes;
-      *reinterpret_cast<uint16_t*>(out + v_code_at<D>(r, d + 4)) = (uint16_t)(codes >> 16);
-    }
-    if (d % 32 == 0) out[is_v ? v_exp_at<D>(r, d / 32) : k_exp_at<D>(r, d / 32)] = (uint8_t)ex;
-  }
 }
 
 template <typename T, int D>
@@ -87,21 +129,28 @@ kept_unpack_kernel(const uint8_t* __restrict__ packed, const int32_t* __restrict
   const int left = ret_count[head] - 32 * blk;
   if (left <= 0) return;
   const uint8_t* in = packed + (head * n_blocks + blk) * (int64_t)PackGeo<D>::kBlock;
-  constexpr int kItems = 2 * 32 * D / 8;
+  constexpr int kEach = 32 * D / 8 / kPackThreads;
+  const int64_t row0 = (head * budget + 32 * blk) * D;
+  const uint32_t bytes = (uint32_t)((left < 32 ? left : 32) * D * (int)sizeof(T));      // rows past them are not written
+  const auto rk = bytes_at(k_ret + row0, bytes), rv = bytes_at(v_ret + row0, bytes);
+  uint32_t codes[2][kEach], ex[2][kEach];
 #pragma unroll
-  for (int i = threadIdx.x; i < kItems; i += kPackThreads) {
-    const int d = 8 * (i % (D / 8)), r = i / (D / 8) % 32;
-    const bool is_v = i >= kItems / 2;
-    if (r >= left) continue;
-    uint32_t codes;
-    if (!is_v || D == 128) codes = *reinterpret_cast<const uint32_t*>(in + (is_v ? v_code_at<D>(r, d) : k_code_at<D>(r, d)));
-    else codes = *reinterpret_cast<const uint16_t*>(in + v_code_at<D>(r, d)) | (uint32_t)*reinterpret_cast<const uint16_t*>(in + v_code_at<D>(r, d + 4)) << 16;
-    const float scale = group_scale(in[is_v ? v_exp_at<D>(r, d / 32) : k_exp_at<D>(r, d / 32)]);
-    float x[8];
+  for (int is_v = 0; is_v < 2; ++is_v)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = code_value(codes >> (4 * e), scale);
-    store8((is_v ? v_ret : k_ret) + (head * budget + 32 * blk + r) * D + d, x);
-  }
+    for (int i = 0; i < kEach; ++i) {
+      const int item = threadIdx.x + i * kPackThreads, d = 8 * (item % (D / 8)), r = item / (D / 8);
+      if (!is_v || D == 128) codes[is_v][i] = *reinterpret_cast<const uint32_t*>(in + (is_v ? v_code_at<D>(r, d) : k_code_at<D>(r, d)));
+      else codes[is_v][i] = *reinterpret_cast<const uint16_t*>(in + v_code_at<D>(r, d)) | (uint32_t)*reinterpret_cast<const uint16_t*>(in + v_code_at<D>(r, d + 4)) << 16;
+      ex[is_v][i] = in[is_v ? v_exp_at<D>(r, d / 32) : k_exp_at<D>(r, d / 32)];
+    }
+#pragma unroll
+  for (int is_v = 0; is_v < 2; ++is_v)
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      Eight<T> x;
+      x.set(codes[is_v][i], __uint_as_float(ex[is_v][i] << 23));
+      x.store(is_v ? rv : rk, (uint32_t)(threadIdx.x + i * kPackThreads) * 8u * (uint32_t)sizeof(T));
+    }
 }
 
 // Workgroups (shares) of a head and their waves.  A launch takes 256 CUs.

@@ -71,15 +71,6 @@ __device__ __forceinline__ Entry first_of_wave(const Entry& x) {
   return Entry{m, __builtin_amdgcn_readlane(x.slot, (int)__builtin_ctzll(at))};
 }
 
-// `bytes` bytes at p, the same in all lanes; what lies past them reads as zeros and is not written.
-__device__ __forceinline__ auto bytes_at(const void* p, uint32_t bytes) {
-  const uint64_t a = reinterpret_cast<uint64_t>(p);        // (the compiler does not see that this is the same in all lanes)
-  void* same = reinterpret_cast<void*>((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) << 32 |
-                                       (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a));
-  return __builtin_amdgcn_make_buffer_rsrc(same, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
-}
-constexpr int kNonTemporal = 2;              // of buffer instructions
-
 // ---- 32 rows of a head in registers ------------------------------------------------------------------------------------------
 // Stored rows.  K: piece i of tile j is 16 bytes of row 8 (c / 4) + 4 j + c % 4 of the block.  V: row 8 kg + u, a lane's channels
 // are D / 16 consecutive ones of the row.
@@ -173,31 +164,6 @@ template <int D> struct PackedRows {
       }
   }
 };
-
-__device__ __forceinline__ uint32_t bf16_pair(uint32_t codes, float scale, int byte) {
-  bf16x2 r;
-  switch (byte) {          // an immediate of the instruction
-    case 0: r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0); break;
-    case 1: r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1); break;
-    case 2: r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2); break;
-    default: r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3); break;
-  }
-  return __builtin_bit_cast(uint32_t, r);
-}
-
-// The same as two fp32 values.
-__device__ __forceinline__ void f32_pair(uint32_t codes, float scale, int byte, float& a, float& b) {
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
-  f32x2 r;
-  switch (byte) {
-    case 0: r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0); break;
-    case 1: r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1); break;
-    case 2: r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2); break;
-    default: r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3); break;
-  }
-  a = r[0];
-  b = r[1];
-}
 
 // ---- scores and outputs of 32 rows --------------------------------------------------------------------------------------------
 // Scores x[u] of row 8 kg + u against the lane's column.  qf: the column's query in the channel order of the rows; bf16: in LDS, this
