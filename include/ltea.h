@@ -377,8 +377,8 @@ int ltea_decode_step_mass(const ltea_cfg *cfg, const void *q, const void *k, con
                           size_t workspace_bytes, void *stream);
 
 /* ltea_decode_step_lazy over a compact segment in 4 bits: keys are the scores that ltea_rescore writes, n_scored is
- * left alone, and a token that leaves the window without a final score is reported as there.  Workspace:
- * ltea_decode_kept_workspace_bytes. */
+ * left alone, and a token that leaves the window without a final score is reported as there.  packed may be NULL where
+ * budget is 0.  Workspace: ltea_decode_kept_workspace_bytes. */
 int ltea_decode_step_packed(const ltea_cfg *cfg, const void *q, const void *k, const void *v, void *out,
                             const ltea_cache *cache, void *packed, int32_t n_seqs, int32_t *status_or_null,
                             void *workspace, size_t workspace_bytes, void *stream);

@@ -514,29 +514,40 @@ def ltea_decode_step_lazy(cfg: ltea_cfg, q: torch.Tensor, k: torch.Tensor, v: to
     return out
 
 
-def _dense(x: torch.Tensor, shape, dtype: torch.dtype, device, what: str) -> None:
-    """A contiguous tensor of exactly this shape and type, on this device."""
-    assert tuple(x.shape) == tuple(shape) and x.dtype == dtype and x.is_contiguous() and x.device == device, \
-        f"{what}: expected a contiguous {tuple(shape)} {dtype} tensor on {device}"
+def _dense(x: torch.Tensor, shape: tuple, dtype: torch.dtype, device: int, what: str) -> None:
+    """A contiguous tensor of exactly this shape and type, on the device of this index."""
+    assert x.shape == shape and x.dtype is dtype and x.is_contiguous() and x.get_device() == device, \
+        f"{what}: expected a contiguous {shape} {dtype} tensor on device {device}, not {tuple(x.shape)} {x.dtype} on {x.device}"
 
 
-def _on_current_device(x: torch.Tensor, what: str) -> None:
-    """Kernels are enqueued on the current device's current stream."""
-    assert x.device.type == "cuda" and x.device.index == torch.cuda.current_device(), \
-        f"{what}: its device ({x.device}) is not the current one"
+def _current_device(x: torch.Tensor, what: str) -> int:
+    """The index of x's device, which has to be the current one: kernels are enqueued on its current stream."""
+    device = x.get_device()
+    assert device >= 0 and device == torch.cuda.current_device(), f"{what}: its device ({x.device}) is not the current one"
+    return device
 
 
-def _views(cfg: ltea_cfg, q: torch.Tensor, cu_seqlens: torch.Tensor, *kv: torch.Tensor) -> int:
-    """Checks of packed [T, H, D] views and their cu_seqlens; returns the number of sequences."""
+def _workspace_of(workspace: Optional[torch.Tensor], device: int, nbytes) -> torch.Tensor:
+    """The caller's workspace, or one of nbytes() bytes."""
+    if workspace is None:
+        return _workspace(nbytes(), device)
+    assert workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.get_device() == device, \
+        f"workspace: expected contiguous bytes on device {device}"
+    return workspace
+
+
+def _views(cfg: ltea_cfg, q: torch.Tensor, cu_seqlens: torch.Tensor, *kv: torch.Tensor):
+    """Checks of packed [T, H, D] views and their cu_seqlens; returns the number of sequences and the device."""
     td = torch.float32 if cfg.dtype == LTEA_F32 else torch.bfloat16
     T = q.shape[0]
-    assert q.dim() == 3 and tuple(q.shape[1:]) == (cfg.Hq, cfg.D) and q.dtype == td, "q: expected [T, Hq, D] of the config's type"
+    assert q.shape == (T, cfg.Hq, cfg.D) and q.dtype is td, "q: expected [T, Hq, D] of the config's type"
+    device = _current_device(q, "q")
     for x in kv:
-        assert tuple(x.shape) == (T, cfg.Hkv, cfg.D) and x.dtype == td and x.device == q.device, "k, v: expected [T, Hkv, D] of the config's type"
-    _dense(cu_seqlens, (cu_seqlens.numel(),), torch.int32, q.device, "cu_seqlens")
-    assert cu_seqlens.numel() >= 1, "cu_seqlens: expected n_seqs + 1 entries"
-    _on_current_device(q, "q")
-    return cu_seqlens.numel() - 1
+        assert x.shape == (T, cfg.Hkv, cfg.D) and x.dtype is td and x.get_device() == device, "k, v: expected [T, Hkv, D] of the config's type"
+    n = cu_seqlens.numel()
+    assert n >= 1, "cu_seqlens: expected n_seqs + 1 entries"
+    _dense(cu_seqlens, (n,), torch.int32, device, "cu_seqlens")
+    return n - 1, device
 
 
 def ltea_mass_workspace_bytes(cfg: ltea_cfg, n_seqs: int, total_tokens: int, max_seqlen: int) -> int:
@@ -549,15 +560,14 @@ def ltea_attention_mass(cfg: ltea_cfg, q: torch.Tensor, k: torch.Tensor, cu_seql
     """The attention weight every token has received from the last `last` queries of its sequence (0: all): [Hkv, T] fp32.
     lse [Hq, T] fp32: the queries' log normalisers, as ltea_train_forward returns them."""
     T = q.shape[0]
-    n_seqs = _views(cfg, q, cu_seqlens, k)
+    n_seqs, device = _views(cfg, q, cu_seqlens, k)
     qst, qsh = _tok_head_strides(q)
     st, sh = _tok_head_strides(k)
-    _dense(lse, (cfg.Hq, T), torch.float32, q.device, "lse")
+    _dense(lse, (cfg.Hq, T), torch.float32, device, "lse")
     if mass is None:
         mass = torch.empty((cfg.Hkv, T), dtype=torch.float32, device=q.device)
-    _dense(mass, (cfg.Hkv, T), torch.float32, q.device, "mass")
-    if workspace is None:
-        workspace = _workspace(ltea_mass_workspace_bytes(cfg, n_seqs, T, max_seqlen), q.device)
+    _dense(mass, (cfg.Hkv, T), torch.float32, device, "mass")
+    workspace = _workspace_of(workspace, device, lambda: ltea_mass_workspace_bytes(cfg, n_seqs, T, max_seqlen))
     _check(lib().ltea_attention_mass(C.byref(cfg), _ptr(q), qst, qsh, _ptr(k), st, sh, _ptr(cu_seqlens), n_seqs, T, max_seqlen,
                                      _ptr(lse), int(last), _ptr(mass), _ptr(workspace), workspace.numel(), _stream()),
            "ltea_attention_mass")
@@ -574,42 +584,41 @@ def ltea_prefill_mass(cfg: ltea_cfg, q: torch.Tensor, k: torch.Tensor, v: torch.
     """Prefill of a cache that keeps the entries with the largest accumulated attention weight; the prompt attends to all of
     itself.  mass (optional, [Hkv, T] fp32) receives the weights."""
     T = q.shape[0]
-    n_seqs = _views(cfg, q, cu_seqlens, k, v)
+    n_seqs, device = _views(cfg, q, cu_seqlens, k, v)
     qst, qsh = _tok_head_strides(q)
     st, sh = _tok_head_strides(k)
     assert _tok_head_strides(v) == (st, sh)
     if out is None:
         out = torch.empty((T, cfg.Hq, cfg.D), dtype=q.dtype, device=q.device)
-    _dense(out, (T, cfg.Hq, cfg.D), q.dtype, q.device, "out")
+    _dense(out, (T, cfg.Hq, cfg.D), q.dtype, device, "out")
     if mass is not None:
-        _dense(mass, (cfg.Hkv, T), torch.float32, q.device, "mass")
-    if workspace is None:
-        workspace = _workspace(ltea_prefill_mass_workspace_bytes(cfg, n_seqs, T, max_seqlen), q.device)
-    _check_cache(cfg, cache, n_seqs, q)
+        _dense(mass, (cfg.Hkv, T), torch.float32, device, "mass")
+    workspace = _workspace_of(workspace, device, lambda: ltea_prefill_mass_workspace_bytes(cfg, n_seqs, T, max_seqlen))
+    _check_cache(cfg, cache, n_seqs, q.dtype, device)
     _check(lib().ltea_prefill_mass(C.byref(cfg), _ptr(q), qst, qsh, _ptr(k), _ptr(v), st, sh, _ptr(cu_seqlens), n_seqs, T,
                                    max_seqlen, int(last), _ptr(out), C.byref(cache.struct), _ptr(mass), _ptr(workspace),
                                    workspace.numel(), _stream()), "ltea_prefill_mass")
     return out
 
 
-def _check_cache(cfg: ltea_cfg, cache: Cache, n_seqs: int, like: torch.Tensor, kept_rows: bool = True) -> None:
+def _check_cache(cfg: ltea_cfg, cache: Cache, n_seqs: int, td: torch.dtype, device: int, kept_rows: bool = True) -> None:
     """Sizes and types of a cache for at least n_seqs sequences."""
-    td, dev = like.dtype, like.device
-    f32, i32 = torch.float32, torch.int32
-    want = [("k_win", (cfg.window, cfg.D), td), ("v_win", (cfg.window, cfg.D), td), ("win_score", (cfg.window,), f32),
-            ("ret_count", (), i32)]
+    n, H, f32, i32 = cache.k_win.shape[0], cfg.Hkv, torch.float32, torch.int32
+    assert n >= n_seqs, f"cache: expected at least {n_seqs} sequences"
+    rows = (n, H, cfg.window, cfg.D)
+    _dense(cache.k_win, rows, td, device, "cache.k_win")
+    _dense(cache.v_win, rows, td, device, "cache.v_win")
+    _dense(cache.win_score, rows[:3], f32, device, "cache.win_score")
+    _dense(cache.ret_count, rows[:2], i32, device, "cache.ret_count")
+    _dense(cache.n_seen, rows[:1], i32, device, "cache.n_seen")
+    _dense(cache.n_scored, rows[:1], i32, device, "cache.n_scored")
     if cfg.budget > 0:
-        want += [("ret_score", (cfg.budget,), f32), ("ret_pos", (cfg.budget,), i32)]
+        rows = (n, H, cfg.budget, cfg.D)
+        _dense(cache.ret_score, rows[:3], f32, device, "cache.ret_score")
+        _dense(cache.ret_pos, rows[:3], i32, device, "cache.ret_pos")
         if kept_rows:
-            want += [("k_ret", (cfg.budget, cfg.D), td), ("v_ret", (cfg.budget, cfg.D), td)]
-    for name, shape, dt in want:
-        x = getattr(cache, name)
-        assert x.dim() >= 2 and x.shape[0] >= n_seqs, f"cache.{name}: expected at least {n_seqs} sequences"
-        _dense(x, (x.shape[0], cfg.Hkv, *shape), dt, dev, f"cache.{name}")
-    for name in ("n_seen", "n_scored"):
-        x = getattr(cache, name)
-        assert x.numel() >= n_seqs, f"cache.{name}: expected at least {n_seqs} sequences"
-        _dense(x, (x.numel(),), i32, dev, f"cache.{name}")
+            _dense(cache.k_ret, rows, td, device, "cache.k_ret")
+            _dense(cache.v_ret, rows, td, device, "cache.v_ret")
 
 
 def ltea_packed_bytes(cfg: ltea_cfg, n_seqs: int) -> int:
@@ -621,16 +630,16 @@ def alloc_packed(cfg: ltea_cfg, n_seqs: int, device="cuda") -> torch.Tensor:
     return torch.zeros((n_seqs, cfg.Hkv, (cfg.budget + 31) // 32, 34 * cfg.D), dtype=torch.uint8, device=device)
 
 
-def _check_packed(cfg: ltea_cfg, packed: torch.Tensor, n_seqs: int, device) -> None:
-    assert packed.dtype == torch.uint8 and packed.is_contiguous() and packed.device == device and \
-        packed.numel() >= ltea_packed_bytes(cfg, n_seqs), "packed: expected the bytes that alloc_packed gives"
+def _check_packed(cfg: ltea_cfg, packed: torch.Tensor, n_seqs: int, device: int) -> None:
+    assert packed.dtype is torch.uint8 and packed.is_contiguous() and packed.get_device() == device and \
+        packed.numel() >= n_seqs * cfg.Hkv * ((cfg.budget + 31) // 32) * 34 * cfg.D, "packed: expected the bytes that alloc_packed gives"
 
 
 def ltea_kept_pack(cfg: ltea_cfg, cache: Cache, packed: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The kept rows of every sequence of `cache` in 4 bits."""
-    n_seqs, dev = cache.ret_count.shape[0], cache.ret_count.device
+    n_seqs = cache.ret_count.shape[0]
     if packed is None:
-        packed = alloc_packed(cfg, n_seqs, dev)
+        packed = alloc_packed(cfg, n_seqs, cache.ret_count.device)
     _convert_kept(cfg, packed, cache, n_seqs)
     _check(lib().ltea_kept_pack(C.byref(cfg), C.byref(cache.struct), _ptr(packed), n_seqs, _stream()), "ltea_kept_pack")
     return packed
@@ -645,13 +654,13 @@ def ltea_kept_unpack(cfg: ltea_cfg, packed: torch.Tensor, cache: Cache) -> Cache
 
 
 def _convert_kept(cfg: ltea_cfg, packed: torch.Tensor, cache: Cache, n_seqs: int) -> None:
-    td, dev = torch.float32 if cfg.dtype == LTEA_F32 else torch.bfloat16, cache.ret_count.device
-    _on_current_device(cache.ret_count, "cache")
-    _check_packed(cfg, packed, n_seqs, dev)
-    _dense(cache.ret_count, (n_seqs, cfg.Hkv), torch.int32, dev, "cache.ret_count")
+    device = _current_device(cache.ret_count, "cache")
+    _check_packed(cfg, packed, n_seqs, device)
+    _dense(cache.ret_count, (n_seqs, cfg.Hkv), torch.int32, device, "cache.ret_count")
     if cfg.budget > 0:
-        for name in ("k_ret", "v_ret"):
-            _dense(getattr(cache, name), (n_seqs, cfg.Hkv, cfg.budget, cfg.D), td, dev, f"cache.{name}")
+        td, rows = torch.float32 if cfg.dtype == LTEA_F32 else torch.bfloat16, (n_seqs, cfg.Hkv, cfg.budget, cfg.D)
+        _dense(cache.k_ret, rows, td, device, "cache.k_ret")
+        _dense(cache.v_ret, rows, td, device, "cache.v_ret")
 
 
 def ltea_decode_kept_workspace_bytes(cfg: ltea_cfg, n_seqs: int) -> int:
@@ -659,20 +668,20 @@ def ltea_decode_kept_workspace_bytes(cfg: ltea_cfg, n_seqs: int) -> int:
 
 
 def _kept_step_tensors(cfg: ltea_cfg, q, k, v, cache, packed, out, workspace):
-    B = q.shape[0]
+    B, D = q.shape[0], cfg.D
     td = torch.float32 if cfg.dtype == LTEA_F32 else torch.bfloat16
-    _on_current_device(q, "q")
-    for x, h, what in ((q, cfg.Hq, "q"), (k, cfg.Hkv, "k"), (v, cfg.Hkv, "v")):
-        _dense(x, (B, h, cfg.D), td, q.device, what)
-    _check_cache(cfg, cache, B, q, packed is None)
+    device = _current_device(q, "q")
+    _dense(q, (B, cfg.Hq, D), td, device, "q")
+    _dense(k, (B, cfg.Hkv, D), td, device, "k")
+    _dense(v, (B, cfg.Hkv, D), td, device, "v")
+    _check_cache(cfg, cache, B, td, device, packed is None)
     if packed is not None:
-        _check_packed(cfg, packed, B, q.device)
+        _check_packed(cfg, packed, B, device)
     if out is None:
-        out = torch.empty((B, cfg.Hq, cfg.D), dtype=td, device=q.device)
-    _dense(out, (B, cfg.Hq, cfg.D), td, q.device, "out")
-    if workspace is None:
-        workspace = _workspace(ltea_decode_kept_workspace_bytes(cfg, B), q.device)
-    return B, out, workspace
+        out = torch.empty((B, cfg.Hq, D), dtype=td, device=q.device)
+    else:
+        _dense(out, (B, cfg.Hq, D), td, device, "out")
+    return B, out, _workspace_of(workspace, device, lambda: ltea_decode_kept_workspace_bytes(cfg, B))
 
 
 def ltea_decode_step_mass(cfg: ltea_cfg, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: Cache,
@@ -690,6 +699,9 @@ def ltea_decode_step_packed(cfg: ltea_cfg, q: torch.Tensor, k: torch.Tensor, v: 
                             out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
                             workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """ltea_decode_step_lazy over kept rows in 4 bits."""
+    assert packed is not None, "packed: expected the kept rows in 4 bits"
+    if status is not None:
+        assert status.numel() >= 1 and status.dtype is torch.int32 and status.get_device() == q.get_device(), "status: expected an int32 on q's device"
     B, out, workspace = _kept_step_tensors(cfg, q, k, v, cache, packed, out, workspace)
     _check(lib().ltea_decode_step_packed(C.byref(cfg), _ptr(q), _ptr(k), _ptr(v), _ptr(out), C.byref(cache.struct), _ptr(packed), B,
                                          _ptr(status), _ptr(workspace), workspace.numel(), _stream()), "ltea_decode_step_packed")

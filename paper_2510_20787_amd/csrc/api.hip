@@ -689,7 +689,7 @@ int ltea_decode_step_mass(const ltea_cfg* cfg, const void* q, const void* k, con
 
 int ltea_decode_step_packed(const ltea_cfg* cfg, const void* q, const void* k, const void* v, void* out, const ltea_cache* cache,
                             void* packed, int32_t n_seqs, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!packed) return LTEA_EINVAL;
+  if (!packed && (!cfg || cfg->budget > 0)) return LTEA_EINVAL;
   return kept_step(cfg, q, k, v, out, cache, packed, false, n_seqs, status, workspace, workspace_bytes, stream);
 }
 

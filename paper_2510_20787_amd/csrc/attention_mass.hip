@@ -242,13 +242,17 @@ attention_mass_kernel(const T* __restrict__ q, int64_t q_st, int64_t q_sh, const
   }
 }
 
+// Tokens that are in no sequence keep what they have.
 __global__ void __launch_bounds__(kThreads)
-mass_parts_kernel(const float* __restrict__ sums, int parts, int64_t n, float* __restrict__ mass) {
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= n) return;
+mass_parts_kernel(const float* __restrict__ sums, int parts, int64_t total, int Hkv, int blocks, const int32_t* __restrict__ cu, int n_seqs,
+                  float* __restrict__ mass) {
+  const int h = blockIdx.x / blocks;
+  const int64_t j = (int64_t)(blockIdx.x - h * blocks) * kThreads + threadIdx.x;
+  if (j < cu[0] || j >= cu[n_seqs]) return;
   float v = 0.f;
-  for (int p = 0; p < parts; ++p) v += sums[p * n + i];
-  mass[i] = v;
+#pragma unroll 4
+  for (int p = 0; p < parts; ++p) v += sums[((int64_t)p * Hkv + h) * total + j];
+  mass[h * total + j] = v;
 }
 
 struct Split { int parts, rows; };
@@ -305,8 +309,9 @@ hipError_t launch_attention_mass(const ltea_cfg& cfg, const void* q, int64_t q_s
                            ? (cfg.D == 64 ? go(float{}, std::integral_constant<int, 64>{}) : go(float{}, std::integral_constant<int, 128>{}))
                            : (cfg.D == 64 ? go(bf16_t{}, std::integral_constant<int, 64>{}) : go(bf16_t{}, std::integral_constant<int, 128>{}));
   if (e != hipSuccess || s.parts == 1) return e;
-  const int64_t n = sv.total_tokens * cfg.Hkv;
-  hipLaunchKernelGGL(mass_parts_kernel, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, sums, s.parts, n, mass);
+  const int blocks = (int)((sv.total_tokens + kThreads - 1) / kThreads);
+  hipLaunchKernelGGL(mass_parts_kernel, dim3((unsigned)(blocks * cfg.Hkv)), dim3(kThreads), 0, stream, sums, s.parts, sv.total_tokens, cfg.Hkv,
+                     blocks, sv.cu_seqlens, sv.n_seqs, mass);
   return hipGetLastError();
 }
 

@@ -80,7 +80,7 @@ kept_pack_kernel(const T* __restrict__ k_ret, const T* __restrict__ v_ret, const
                  int n_blocks, uint8_t* __restrict__ packed) {
   const int64_t head = blockIdx.x / n_blocks;
   const int blk = (int)(blockIdx.x - head * n_blocks);
-  const int left = ret_count[head] - 32 * blk;
+  const int count = ret_count[head], left = (count < budget ? count : budget) - 32 * blk;
   if (left <= 0) return;
   uint8_t* out = packed + (head * n_blocks + blk) * (int64_t)PackGeo<D>::kBlock;
   constexpr int kEach = 32 * D / 8 / kPackThreads;          // items of K, and of V, per thread
@@ -126,7 +126,7 @@ kept_unpack_kernel(const uint8_t* __restrict__ packed, const int32_t* __restrict
                    T* __restrict__ k_ret, T* __restrict__ v_ret) {
   const int64_t head = blockIdx.x / n_blocks;
   const int blk = (int)(blockIdx.x - head * n_blocks);
-  const int left = ret_count[head] - 32 * blk;
+  const int count = ret_count[head], left = (count < budget ? count : budget) - 32 * blk;
   if (left <= 0) return;
   const uint8_t* in = packed + (head * n_blocks + blk) * (int64_t)PackGeo<D>::kBlock;
   constexpr int kEach = 32 * D / 8 / kPackThreads;
