@@ -471,14 +471,13 @@ __device__ __forceinline__ void grow_keys(const CacheDev& C, const KeptParams& P
   if (dst >= 32 * sh.kept0 && dst < k1 && tid == 0) C.ret_pos[head * P.budget + dst] = p.leaving;
 }
 
-// The leaving token's row to its slot, the incoming token's into the ring.  Threads 0 .. D - 1.
+// The leaving token's row (ke, ve) to its slot, the incoming token's into the ring.  Threads 0 .. D - 1, a channel each.
 template <typename T, int D, bool PK>
-__device__ __forceinline__ void move_rows(const CacheDev& C, const KeptParams& P, const Plan& p, int64_t head, int dst, T k_in, T v_in) {
+__device__ __forceinline__ void move_rows(const CacheDev& C, const KeptParams& P, const Plan& p, int64_t head, int dst, T ke, T ve, T k_in, T v_in) {
   const int d = threadIdx.x;
   T* kw = static_cast<T*>(C.k_win) + (head * P.window + p.slot) * D;
   T* vw = static_cast<T*>(C.v_win) + (head * P.window + p.slot) * D;
   if (dst >= 0) {
-    const T ke = kw[d], ve = vw[d];
     if constexpr (PK) {
       uint8_t* block = const_cast<uint8_t*>(P.packed) + (head * ((P.budget + 31) / 32) + dst / 32) * (int64_t)PackGeo<D>::kBlock;
       const int r = dst % 32;
@@ -592,7 +591,7 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
   __shared__ Entry red_e[W];
   __shared__ float ve_lds[D];
   __shared__ __align__(16) u32x4 q_lds[sizeof(T) == 2 ? (PK ? 2 : 1) * kQ * kWave : 1];      // bf16: a pass's queries as B operands, [rows, packed rows][piece][lane]
-  __shared__ __align__(16) T rows_lds[3][D];          // keys of the incoming and of the leaving token, the latter's value
+  __shared__ __align__(16) T rows_lds[4][D];          // keys of the incoming and of the leaving token, the latter's value, the former's
   static_assert(sizeof(red_m) + sizeof(red_l) + sizeof(red_e) + sizeof(ve_lds) + sizeof(q_lds) + sizeof(rows_lds) + kKeptLds <= 64 * 1024, "LDS");
   const int tid = threadIdx.x, lane = tid & (kWave - 1), c = lane & 15, kg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -681,8 +680,8 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
   read_here(z_e);
   const Plan p = plan_of(P, t, count, z_e, late);
   // rows that are needed at the end, straight into LDS
-  if (wave < 3 && lane < D * (int)sizeof(T) / 16) {
-    const T* row = wave == 0 ? k_new + head * D : (wave == 1 ? kw : vw) + (int64_t)p.slot * D;
+  if (wave < 4 && lane < D * (int)sizeof(T) / 16) {
+    const T* row = wave == 0 ? k_new + head * D : wave == 3 ? v_new + head * D : (wave == 1 ? kw : vw) + (int64_t)p.slot * D;
     dma16(make_raw_rsrc(row, (uint32_t)(D * sizeof(T))), (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)&rows_lds[wave][0], 16u * (uint32_t)lane);
   }
 
@@ -883,7 +882,7 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
       if (whole) {
         const float w_t = exp2_hw(fmaf(xs[g], P.scale2, -ref)), w_e = dst >= 0 ? exp2_hw(fmaf(xs[G + g], P.scale2, -ref)) : 0.f;
         L += w_t + w_e;
-        A = fmaf(w_t, to_f32(v_new[head * D + d]), A);
+        A = fmaf(w_t, to_f32(rows_lds[3][d]), A);
         if (dst >= 0) A = fmaf(w_e, ve_lds[d], A);
         if (d == 0) { top[g] = ref; inv[g] = 1.0f / L; }
         out[((int64_t)b * P.Hq + h * G + g) * D + d] = from_f32<T>(late ? __builtin_nanf("") : A / L);
@@ -940,7 +939,7 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
     return;
   }
   // every row has been read
-  if (tid < D) move_rows<T, D, PK>(C, P, p, head, dst, k_new[head * D + tid], v_new[head * D + tid]);
+  if (tid < D) move_rows<T, D, PK>(C, P, p, head, dst, rows_lds[1][tid], rows_lds[2][tid], rows_lds[0][tid], rows_lds[3][tid]);
   if (tid == 0) {
     unsigned* words = reinterpret_cast<unsigned*>(C.ret_count + (int64_t)b * P.Hkv);
     if (dst >= 0 && dst == count) atomicAdd(words + h, 1u);
@@ -982,6 +981,13 @@ kept_finish_kernel(CacheDev C, KeptParams P, const T* __restrict__ k_new, const 
   take_shares<D>(P, rec, i0 < items ? i0 / D : 0, i0 % D, 0, F);
   request_keys(C, P, head, sh, first);
   request_scores(P, sh, first, score4);
+  T ke = T(0), ve = T(0), k_in = T(0), v_in = T(0);
+  if (split == 0 && tid < D) {
+    ke = static_cast<const T*>(C.k_win)[(head * P.window + p.slot) * D + tid];
+    ve = static_cast<const T*>(C.v_win)[(head * P.window + p.slot) * D + tid];
+    k_in = k_new[head * D + tid];
+    v_in = v_new[head * D + tid];
+  }
   const int dst = join_shares<D>(P, p, rec, xs, fac, stay, top, inv);
   __syncthreads();
   for (int i = i0; i < i1; i += kStepThreads) {
@@ -992,7 +998,7 @@ kept_finish_kernel(CacheDev C, KeptParams P, const T* __restrict__ k_new, const 
   }
   grow_keys<kStepThreads>(C, P, p, head, sh, dst, xs, top, inv, first, true, score4);
   if (split != 0) return;
-  if (tid < D) move_rows<T, D, PK>(C, P, p, head, dst, k_new[head * D + tid], v_new[head * D + tid]);
+  if (tid < D) move_rows<T, D, PK>(C, P, p, head, dst, ke, ve, k_in, v_in);
   if (tid == 0) {
     if (dst >= 0 && dst == p.count) C.ret_count[head] = p.count + 1;
     if (h == 0) {
