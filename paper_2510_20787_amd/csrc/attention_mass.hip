@@ -2,10 +2,15 @@
 // that see j of exp(scale q_i . k_j - lse_i).
 //
 //   S[key, query] = K . Q^T    v_mfma_f32_32x32x16_bf16 (fp32: v_mfma_f32_32x32x2_f32), K held in registers for the life of a wave,
-//                              Q tiles of 64 rows through LDS
+//                              Q tiles of 128 rows (fp32: 64) through LDS
 //   mass[key] += 2^(S c - lse_i log2(e))
 // A lane owns one query column, so lse is one register, and keeps sums of its 16 keys per block that meet over the lanes once, at
 // the end.  Products of bf16 values are exact in fp32 and nothing is rounded to fewer bits.
+//
+// Bound: a wave's issue.  32 x 32 scores take 128 cycles of exponentials and 128 of scale and sum beside 64 (D = 64) or 128 (D = 128)
+// of matrix instructions, which overlap little: 4 x 4096 tokens, 32/8 heads, D = 64: 223 us (615 TFLOP/s of products), 32768 tokens, 32
+// heads, D = 128: 4263 us (1.03 PFLOP/s).  Two blocks of 32 keys per wave: at D = 64 three take 271 us and four 342 (fewer waves);
+// 16 x 16 instructions 8515 us for the long prompt where these took 4560 at the time (registers).
 //
 // A workgroup takes 4 waves x KB blocks of 32 keys of one (sequence, KV head) and a part of the queries that can see them, all
 // query heads of the group.  Parts meet in a second launch, in their order: same bits every time, and sums of at most 2048 queries

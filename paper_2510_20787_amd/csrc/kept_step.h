@@ -6,8 +6,9 @@
 //   out = sum_j p_j v_j over ring and kept entries as they are then, p_j = 2^(x_j - M) / L;
 //   by accumulated weight, every entry's key grows by the sum of its p_j over the group's query heads.
 //
-// A workgroup of four waves streams one share of a head's rows as they lie, blocks of 32 ring rows and of 32 kept rows, its waves
-// taking blocks in turn with a running maximum, sum and output each; the scores of all rows are kept (in LDS, or in the workspace).
+// A workgroup of four or eight waves streams a head's rows, or one share of them, as they lie: blocks of 32 ring rows and of 32 kept
+// rows, its waves taking blocks in turn with a running maximum, sum and output each; by accumulated weight, the scores of all rows are
+// kept (in LDS, or in the workspace).
 // Two rows are left out of the stream, because what is at their place differs before and after the step: the ring slot t % window,
 // and the entry that e displaces.  What replaces them, e as it would be kept and the incoming token, joins the softmax at the end;
 // with the normaliser known every key of the head grows by its weight, and the rows move.
