@@ -157,8 +157,8 @@ kept_unpack_kernel(const uint8_t* __restrict__ packed, const int32_t* __restrict
 // More heads than CUs: a head's workgroup of four waves, several of them on a CU (1024 heads of 1024 + 512 rows, D = 128: 136 us, with
 // eight waves 156; 512 heads of packed rows 86 and 99).  As many or fewer: eight waves (256 heads of 512 + 8192 packed rows, D = 128:
 // 73 us, with four 85).
-// Few heads of 64 blocks of rows or more are cut: 8 heads of 768 + 16384 packed rows 23 us in 16 shares, 75 whole.  The second launch
-// costs about 3 us and reading the shares grows with them: 8 heads of 768 + 512 rows 16.5 us whole, 18 in 3, 5 or 8 shares; 8 of
+// Few heads of 64 blocks of rows or more are cut: 8 heads of 768 + 16384 packed rows 21 us in 16 shares, 75 whole.  The second launch
+// costs some 2 us and reading the shares grows with them: 8 heads of 768 + 512 rows 16.5 us whole, 18 in 3, 5 or 8 shares; 8 of
 // 768 + 32768 packed 35, 32, 32, 31, 38 and 47 us in 12, 16, 24, 32, 40 and 64; and where a head gets fewer than four CUs packed rows
 // do not gain (128 heads of 1024 + 8192: 46 us whole, 54 and 49 in 2 and 3), stored ones do (128 of 1024 + 2048: 58 whole, 46 in 2).
 constexpr int64_t kCus = 256;

@@ -361,11 +361,12 @@ template <typename T, int D, bool PK> __device__ __forceinline__ void load_kept_
 }
 
 // ---- the step -----------------------------------------------------------------------------------------------------------------------
+// (Quotients of 32 bits: a head has fewer than 2^24 blocks and at most 64 shares.)
 struct Share { int ring0, ring1, kept0, kept1; };      // blocks of 32 rows
+__device__ __forceinline__ int part_of(int x, int split, int n) { return (int)((uint32_t)x * (uint32_t)split / (uint32_t)n); }
 __device__ __forceinline__ Share share_of(const KeptParams& P, int split) {
-  const int rb = (P.window + 31) / 32, kb = (P.budget + 31) / 32, n = P.L.nsplit;
-  return Share{(int)((int64_t)rb * split / n), (int)((int64_t)rb * (split + 1) / n), (int)((int64_t)kb * split / n),
-               (int)((int64_t)kb * (split + 1) / n)};
+  const int rb = (int)(((uint32_t)P.window + 31u) / 32u), kb = (int)(((uint32_t)P.budget + 31u) / 32u), n = P.L.nsplit;
+  return Share{part_of(rb, split, n), part_of(rb, split + 1, n), part_of(kb, split, n), part_of(kb, split + 1, n)};
 }
 
 // What a step is about, the same in all workgroups of a head.
@@ -513,21 +514,33 @@ __device__ __forceinline__ void advance(const CacheDev& C, const KeptParams& P, 
 
 // What all shares of a head have handed over becomes factors: fac [G][n] of the shares' outputs, stay [G][n] weights of their lowest
 // entries that stay (both relative to 2^top), top [G], inv [G] = 1 / sum.  Returns the slot the leaving token goes to.
+struct FirstRecord { float order_hi, order_lo, slot, x, m, l, x_in, x_out; };      // of the lane's share and the wave's first query head: requested ahead
+template <int D> __device__ __forceinline__ FirstRecord request_record(const KeptParams& P, const float* rec, const float* xs) {
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+  const int n = P.L.nsplit, G = P.L.G, g = wave < G ? wave : 0;
+  const float* r = rec + (lane < n ? lane : 0) * P.L.share();
+  const float* o = r + 4 + G + D + (size_t)g * (D + 2);
+  return FirstRecord{r[0], r[1], r[2], r[4 + g], o[0], o[1], xs[g], xs[G + g]};
+}
 template <int D>
-__device__ __forceinline__ int join_shares(const KeptParams& P, const Plan& p, const float* rec, const float* xs, float* fac, float* stay,
-                                           float* top, float* inv) {
+__device__ __forceinline__ int join_shares(const KeptParams& P, const Plan& p, const float* rec, const float* xs, const FirstRecord& first,
+                                           float* fac, float* stay, float* top, float* inv) {
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const int n = P.L.nsplit, G = P.L.G;
   const float* r = rec + (lane < n ? lane : 0) * P.L.share();
-  Entry mine = {(unsigned long long)__float_as_uint(r[0]) << 32 | __float_as_uint(r[1]), __float_as_int(r[2])};
+  Entry mine = {(unsigned long long)__float_as_uint(first.order_hi) << 32 | __float_as_uint(first.order_lo), __float_as_int(first.slot)};
   if (lane >= n) mine = Entry{~0ull, -1};
   const int dst = target_of(P, p, first_of_wave(mine));
   const bool stays = mine.slot >= 0 && mine.slot != dst;
   for (int g = wave; g < G; g += kStepWaves) {
-    const float* o = r + 4 + G + D + (size_t)g * (D + 2);
-    const float m = lane < n ? o[0] : -INFINITY, l = lane < n ? o[1] : 0.f;
-    const float x_s = stays ? r[4 + g] * P.scale2 : -INFINITY, x_t = xs[g] * P.scale2;
-    const float x_e = dst >= 0 ? xs[G + g] * P.scale2 : -INFINITY;
+    float x = first.x, m = first.m, l = first.l, x_in = first.x_in, x_out = first.x_out;
+    if (g != wave) {
+      const float* o = r + 4 + G + D + (size_t)g * (D + 2);
+      x = r[4 + g]; m = o[0]; l = o[1]; x_in = xs[g]; x_out = xs[G + g];
+    }
+    if (lane >= n) { m = -INFINITY; l = 0.f; }
+    const float x_s = stays ? x * P.scale2 : -INFINITY, x_t = x_in * P.scale2;
+    const float x_e = dst >= 0 ? x_out * P.scale2 : -INFINITY;
     const float M = fmaxf(fmaxf(wave_max(fmaxf(m, x_s)), x_t), x_e);
     const float ref = M == -INFINITY ? 0.f : M;
     const float f = exp2_hw(m - ref), w_s = exp2_hw(x_s - ref);
@@ -596,9 +609,11 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
   static_assert(sizeof(red_m) + sizeof(red_l) + sizeof(red_e) + sizeof(ve_lds) + sizeof(q_lds) + sizeof(rows_lds) + kKeptLds <= 64 * 1024, "LDS");
   const int tid = threadIdx.x, lane = tid & (kWave - 1), c = lane & 15, kg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int n = WHOLE ? 1 : P.L.nsplit, split = WHOLE ? 0 : blockIdx.x % n, G = P.L.G;
-  const int64_t head = WHOLE ? blockIdx.x : blockIdx.x / n;
-  const int b = (int)(head / P.Hkv), h = (int)(head - (int64_t)b * P.Hkv);
+  const int n = WHOLE ? 1 : P.L.nsplit, G = P.L.G;
+  const uint32_t flat = WHOLE ? blockIdx.x : blockIdx.x / (uint32_t)n;
+  const int split = WHOLE ? 0 : (int)(blockIdx.x - flat * (uint32_t)n);
+  const int64_t head = flat;
+  const int b = (int)(flat / (uint32_t)P.Hkv), h = (int)(flat - (uint32_t)b * (uint32_t)P.Hkv);
   const int heads_at_once = G < GT ? G : GT;
   float* red_o = lds;
   float* xs = red_o + W * heads_at_once * kRow;
@@ -606,7 +621,7 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
   float* inv = top + G;
   float* low_x = inv + G;
   float* rest = xs + (6 * G + 3) / 4 * 4;        // 16-byte aligned
-  const Share sh = share_of(P, split);
+  const Share sh = WHOLE ? Share{0, (int)(((uint32_t)P.window + 31u) / 32u), 0, (int)(((uint32_t)P.budget + 31u) / 32u)} : share_of(P, split);
   const T* kw = static_cast<const T*>(C.k_win) + head * P.window * D;
   const T* vw = static_cast<const T*>(C.v_win) + head * P.window * D;
   const T* kr = static_cast<const T*>(C.k_ret) + head * P.budget * D;
@@ -961,9 +976,11 @@ __global__ void __launch_bounds__(kStepThreads)
 kept_finish_kernel(CacheDev C, KeptParams P, const T* __restrict__ k_new, const T* __restrict__ v_new, T* __restrict__ out) {
   extern __shared__ __align__(16) float lds[];
   const int tid = threadIdx.x;
-  const int n = P.L.nsplit, split = blockIdx.x % n, G = P.L.G;
-  const int64_t head = blockIdx.x / n;
-  const int b = (int)(head / P.Hkv), h = (int)(head - (int64_t)b * P.Hkv);
+  const int n = P.L.nsplit, G = P.L.G;
+  const uint32_t flat = blockIdx.x / (uint32_t)n;
+  const int split = (int)(blockIdx.x - flat * (uint32_t)n);
+  const int64_t head = flat;
+  const int b = (int)(flat / (uint32_t)P.Hkv), h = (int)(flat - (uint32_t)b * (uint32_t)P.Hkv);
   const float* plan = P.plan + head * P.L.plan();
   const float* rec = P.shares + head * n * P.L.share();
   const float* scores = P.scores + head * P.L.scores();
@@ -971,19 +988,22 @@ kept_finish_kernel(CacheDev C, KeptParams P, const T* __restrict__ k_new, const 
   float* stay = fac + G * n;
   float* top = stay + G * n;
   float* inv = top + G;
-  const Plan p = plan_of(P, __float_as_int(plan[0]), __float_as_int(plan[1]), plan[2], __float_as_int(plan[3]) != 0);
   const float* xs = plan + 4;
   const Share sh = share_of(P, split);
   const auto from = bytes_at(scores, (uint32_t)(P.L.scores() * sizeof(float)));
   auto score4 = [&](int g, int at) {
     return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, (uint32_t)(g * P.L.slots + at) * 4u, 0, 0));
   };
-  const int items = G * D, i0 = (int)((int64_t)items * split / n) + tid, i1 = (int)((int64_t)items * (split + 1) / n);
+  const int items = G * D, i0 = part_of(items, split, n) + tid, i1 = part_of(items, split + 1, n);
+  // everything whose place is known is requested before anything is waited for
+  const FirstRecord record = request_record<D>(P, rec, xs);
   FirstShares F;
   FirstRows first;
-  take_shares<D>(P, rec, i0 < items ? i0 / D : 0, i0 % D, 0, F);
   request_keys(C, P, head, sh, first);
   request_scores(P, sh, first, score4);
+  const float plan_t = plan[0], plan_count = plan[1], plan_z = plan[2], plan_late = plan[3];
+  take_shares<D>(P, rec, i0 < items ? i0 / D : 0, i0 % D, 0, F);
+  const Plan p = plan_of(P, __float_as_int(plan_t), __float_as_int(plan_count), plan_z, __float_as_int(plan_late) != 0);
   T ke = T(0), ve = T(0), k_in = T(0), v_in = T(0);
   if (split == 0 && tid < D) {
     ke = static_cast<const T*>(C.k_win)[(head * P.window + p.slot) * D + tid];
@@ -991,7 +1011,7 @@ kept_finish_kernel(CacheDev C, KeptParams P, const T* __restrict__ k_new, const 
     k_in = k_new[head * D + tid];
     v_in = v_new[head * D + tid];
   }
-  const int dst = join_shares<D>(P, p, rec, xs, fac, stay, top, inv);
+  const int dst = join_shares<D>(P, p, rec, xs, record, fac, stay, top, inv);
   __syncthreads();
   for (int i = i0; i < i1; i += kStepThreads) {
     const int g = i / D, d = i - g * D;
