@@ -155,22 +155,24 @@ kept_unpack_kernel(const uint8_t* __restrict__ packed, const int32_t* __restrict
 
 // Workgroups (shares) of a head and their waves.  A launch takes 256 CUs.
 // More heads than CUs: a head's workgroup of four waves, several of them on a CU (1024 heads of 1024 + 512 rows, D = 128: 136 us, with
-// eight waves 156; 512 heads of packed rows 86 and 99).  As many or fewer: eight waves (256 heads of 512 + 8192 packed rows, D = 128:
-// 73 us, with four 85).
-// Few heads of 64 blocks of rows or more are cut: 8 heads of 768 + 16384 packed rows 21 us in 16 shares, 75 whole.  The second launch
-// costs some 2 us and reading the shares grows with them: 8 heads of 768 + 512 rows 16.5 us whole, 18 in 3, 5 or 8 shares; 8 of
-// 768 + 32768 packed 35, 32, 32, 31, 38 and 47 us in 12, 16, 24, 32, 40 and 64; and where a head gets fewer than four CUs packed rows
-// do not gain (128 heads of 1024 + 8192: 46 us whole, 54 and 49 in 2 and 3), stored ones do (128 of 1024 + 2048: 58 whole, 46 in 2).
+// eight waves 156; 512 heads of packed rows 86 and 99).  Fewer: eight waves (256 heads of 512 + 8192 packed rows, D = 128: 73 us, with
+// four 85), but four for few short heads (8 heads of 768 + 512 rows 15.4 us, with eight 16.3; 64 heads 17.5 and 17.8).
+// Few heads of 48 blocks of rows or more are cut, in 8 shares or a power of two that leaves each 16 blocks: 8 heads of 768 + 1024 rows 16.1
+// us in 8 (whole 18.2, in 5 17.0), 32 of 768 + 2001 packed 15.7 in 8 (whole 20.6, in 6 and 10 16.5 and 17.4), 8 of 768 + 16384 packed 21.3
+// in 16 and 21.0 in 32 (whole 73.9, in 8 26.5), 8 of 768 + 32768 packed 23.4 in 32 (in 16 and 64 27.2 and 30.4: reading the shares grows
+// with them).  Shorter heads do not gain (40 blocks: 15.4 us whole and in 8).  Where a head gets fewer than four CUs packed rows do
+// not gain either (128 heads of 1024 + 8192: 45 us whole, 47 in 2), stored ones do (128 of 1024 + 2048: 55 whole, 43 in 2).
 constexpr int64_t kCus = 256;
 KeptSplit split_of(const ltea_cfg& cfg, int n_seqs, bool packed) {
   const int64_t heads = (int64_t)n_seqs * cfg.Hkv, G = cfg.Hq / cfg.Hkv, fill = kCus / heads;
+  const int64_t blocks = (int64_t)kept_blocks_of(cfg.window) + kept_blocks_of(cfg.budget);
   if (fill < 1) return KeptSplit{1, 4};
+  if (blocks < 48 || fill < (packed ? 4 : 2)) return KeptSplit{1, blocks < 64 && fill > 2 ? 4 : 8};
   const int64_t row = 2 * cfg.D * (cfg.dtype == LTEA_F32 ? 4 : 2), kept = packed ? 2 * (cfg.D / 2 + cfg.D / 32) : row;
-  const int64_t blocks = (int64_t)kept_blocks_of(cfg.window) + kept_blocks_of(cfg.budget), bytes = cfg.window * row + cfg.budget * kept;
-  if (blocks < 64 || fill < (packed ? 4 : 2)) return KeptSplit{1, 8};
-  const int64_t by_bytes = bytes / (256 * 1024), most = by_bytes < 16 ? 16 : by_bytes, by_lds = kKeptMaxFactors / G;
-  int64_t n = blocks / 10;
-  for (const int64_t limit : {fill, most, by_lds, (int64_t)kKeptMaxShares}) n = n < limit ? n : limit;
+  const int64_t by_bytes = (cfg.window * row + cfg.budget * kept) / (256 * 1024), by_blocks = blocks / 16 < 32 ? blocks / 16 : 32;
+  int64_t n = 8;                   // (by_bytes: wide rows of one or two heads)
+  while (2 * n <= (by_bytes > by_blocks ? by_bytes : by_blocks)) n *= 2;
+  for (const int64_t limit : {fill, kKeptMaxFactors / G, (int64_t)kKeptMaxShares}) n = n < limit ? n : limit;
   return KeptSplit{(int)n, 4};
 }
 

@@ -11,7 +11,8 @@ from tests.kept_util import f64, make_state, run_and_check
 pytestmark = pytest.mark.gpu
 
 # sequences, KV heads, window, budget, heads checked: every n-th
-HEADS = {"four waves": (150, 2, 45, 70, 29), "eight waves": (20, 2, 70, 100, 7), "shares": (2, 2, 100, 2300, 1)}
+HEADS = {"four waves": (150, 2, 45, 70, 29), "few on four waves": (20, 2, 70, 100, 7), "eight waves": (70, 2, 70, 100, 23),
+         "shares": (2, 2, 100, 2300, 1)}
 
 
 @pytest.mark.parametrize("packed", [False, True], ids=["rows", "packed"])
@@ -33,7 +34,7 @@ def test_forms_of_the_step(form, D, G, packed):
 
 @pytest.mark.parametrize("packed", [False, True], ids=["rows", "packed"])
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("nb,Hkv,window,budget,every", [(140, 2, 9, 40, 31), (1, 2, 33, 2500, 1)])
+@pytest.mark.parametrize("nb,Hkv,window,budget,every", [(140, 2, 9, 40, 31), (60, 2, 9, 40, 17), (1, 2, 33, 2500, 1)])
 def test_forms_of_the_step_in_fp32(nb, Hkv, window, budget, every, D, packed):
     cfg = B.make_cfg(3 * Hkv, Hkv, D, window, budget, 0, 0.0, 0.0, "f32")
     cache = make_state(cfg, [window + budget + i for i in range(nb)], [budget] * nb, 32)
