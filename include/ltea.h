@@ -369,8 +369,9 @@ int ltea_kept_unpack(const ltea_cfg *cfg, const void *packed, const ltea_cache *
 /* One decode step that evicts by accumulated weight: steps 2 to 4 of ltea_decode_step with the keys above, after which
  * the key of every ring and compact entry grows by the weight that q_t's softmax gives it (the incoming token starts
  * at zero; a weight that is not a number counts nothing), and n_scored = n_seen.  packed_or_null: the compact rows are
- * there (k_ret, v_ret may then be NULL); the evicted token is attended as it is kept.  At most 128 query heads per KV
- * head, LTEA_EUNSUPPORTED beyond.  Concurrent calls on the same cache or the same workspace race. */
+ * there (k_ret, v_ret may then be NULL); the evicted token is attended as it is kept.  LTEA_EUNSUPPORTED: more than 128
+ * query heads per KV head, more than 2^24 (sequence, KV head) pairs, or 4 * (Hq / Hkv) * (window + budget) of 2^31 bytes and
+ * more.  Concurrent calls on the same cache or the same workspace race. */
 size_t ltea_decode_kept_workspace_bytes(const ltea_cfg *cfg, int32_t n_seqs);
 int ltea_decode_step_mass(const ltea_cfg *cfg, const void *q, const void *k, const void *v, void *out,
                           const ltea_cache *cache, void *packed_or_null, int32_t n_seqs, void *workspace,

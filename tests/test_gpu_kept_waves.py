@@ -43,6 +43,19 @@ def test_forms_of_the_step_in_fp32(nb, Hkv, window, budget, every, D, packed):
         run_and_check(cfg, cache, pk, True, 520 + step, "f32", heads=every)
 
 
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+def test_given_keys_without_a_budget(dtype, D):
+    """Nothing is ever kept, and there are no packed rows to point at."""
+    cfg = B.make_cfg(4, 2, D, 33, 0, 2, 0.0, 0.0, dtype)
+    cache = make_state(cfg, [0, 7, 33, 200], [0, 0, 0, 0], 34)
+    cache.n_scored += 33
+    packed = B.alloc_packed(cfg, 4)
+    assert packed.numel() == 0
+    for step in range(3):
+        run_and_check(cfg, cache, packed, False, 530 + step, dtype)
+    assert B.ltea_kept_pack(cfg, cache).numel() == 0
+
+
 def test_weights_of_many_short_prompts():
     """More sequences than a wave looks up at once, most of a few tokens, some of none."""
     rng = np.random.default_rng(33)
