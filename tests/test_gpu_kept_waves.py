@@ -75,3 +75,15 @@ def test_weights_of_many_short_prompts():
     got = f64(B.ltea_attention_mass(cfg, q, k, cu, 140, torch.from_numpy(lse).float().cuda(), last=3))
     # as for longer prompts: 2^-15 of a weight
     assert (np.abs(got - want) <= 2.0 ** -15 * want + 1e-30).all()
+
+
+def test_prompts_of_no_tokens_start_a_cache():
+    cfg = B.make_cfg(4, 2, 64, 16, 20, 1, 0.0, 0.0, "bf16")
+    cache = make_state(cfg, [50, 60], [20, 20], 35)
+    q, k = [torch.empty((0, h, 64), dtype=torch.bfloat16, device="cuda") for h in (4, 2)]
+    cu = torch.zeros(3, dtype=torch.int32, device="cuda")
+    out = B.ltea_prefill_mass(cfg, q, k, k, cu, 0, cache)
+    assert out.shape == (0, 4, 64) and not cache.n_seen.any() and not cache.n_scored.any() and not cache.ret_count.any()
+    assert B.ltea_attention_mass(cfg, q, k, cu, 0, torch.empty((4, 0), device="cuda")).shape == (2, 0)
+    for step in range(2):
+        run_and_check(cfg, cache, None, True, 540 + step, "bf16")
