@@ -160,7 +160,8 @@ kept_unpack_kernel(const uint8_t* __restrict__ packed, const int32_t* __restrict
 // Few heads of 48 blocks of rows or more are cut, in 8 shares or a power of two that leaves each 16 blocks: 8 heads of 768 + 1024 rows 16.1
 // us in 8 (whole 18.2, in 5 17.0), 32 of 768 + 2001 packed 15.7 in 8 (whole 20.6, in 6 and 10 16.5 and 17.4), 8 of 768 + 16384 packed 21.3
 // in 16 and 21.0 in 32 (whole 73.9, in 8 26.5), 8 of 768 + 32768 packed 23.4 in 32 (in 16 and 64 27.2 and 30.4: reading the shares grows
-// with them).  Shorter heads do not gain (40 blocks: 15.4 us whole and in 8).  Where a head gets fewer than four CUs packed rows do
+// with them); wide rows in more, a share for each 128 KB (2 heads of 768 + 4000 fp32 rows, D = 128: 22.7 us in 32, 25.9 in 16, 25.0 in 64;
+// 4 of 768 + 16384: 33.4 in 64, 37.7 in 32).  Shorter heads do not gain (40 blocks: 15.4 us whole and in 8).  Where a head gets fewer than four CUs packed rows do
 // not gain either (128 heads of 1024 + 8192: 45 us whole, 47 in 2), stored ones do (128 of 1024 + 2048: 55 whole, 43 in 2).
 constexpr int64_t kCus = 256;
 KeptSplit split_of(const ltea_cfg& cfg, int n_seqs, bool packed) {
@@ -169,8 +170,8 @@ KeptSplit split_of(const ltea_cfg& cfg, int n_seqs, bool packed) {
   if (fill < 1) return KeptSplit{1, 4};
   if (blocks < 48 || fill < (packed ? 4 : 2)) return KeptSplit{1, blocks < 64 && fill > 2 ? 4 : 8};
   const int64_t row = 2 * cfg.D * (cfg.dtype == LTEA_F32 ? 4 : 2), kept = packed ? 2 * (cfg.D / 2 + cfg.D / 32) : row;
-  const int64_t by_bytes = (cfg.window * row + cfg.budget * kept) / (256 * 1024), by_blocks = blocks / 16 < 32 ? blocks / 16 : 32;
-  int64_t n = 8;                   // (by_bytes: wide rows of one or two heads)
+  const int64_t by_bytes = (cfg.window * row + cfg.budget * kept) / (128 * 1024), by_blocks = blocks / 16 < 32 ? blocks / 16 : 32;
+  int64_t n = 8;
   while (2 * n <= (by_bytes > by_blocks ? by_bytes : by_blocks)) n *= 2;
   for (const int64_t limit : {fill, kKeptMaxFactors / G, (int64_t)kKeptMaxShares}) n = n < limit ? n : limit;
   return KeptSplit{(int)n, 4};
