@@ -35,7 +35,7 @@ int64_t tile_keys(const ltea_cfg& cfg) {
 }
 
 struct MassParams {
-  int n_seqs, tiles_upper, Hq, Hkv, window, last, parts, part_rows, units;
+  int n_seqs, tiles_upper, Hq, Hkv, window, last, parts, part_rows, head_parts, part_heads, units;
   int64_t total;
   float scale2;
 };
@@ -71,8 +71,8 @@ attention_mass_kernel(const T* __restrict__ q, int64_t q_st, int64_t q_sh, const
   if (!locate_tile(cu, P.n_seqs, kKeys, flat, seq, tile_i, lo, n)) return;
   const int key0 = tile_i * kKeys, key1 = key0 + kKeys < n ? key0 + kKeys : n;
   int q0, q1;
-  queries_of(P, part, n, key0, key1, q0, q1);
-  const int G = P.Hq / P.Hkv;
+  queries_of(P, part / P.head_parts, n, key0, key1, q0, q1);
+  const int G = P.Hq / P.Hkv, g0 = part % P.head_parts * P.part_heads, g1 = g0 + P.part_heads < G ? g0 + P.part_heads : G;
 
   float* to = sums + ((int64_t)part * P.Hkv + h) * P.total + lo;
   if (q1 <= q0) {
@@ -149,14 +149,14 @@ attention_mass_kernel(const T* __restrict__ q, int64_t q_st, int64_t q_sh, const
 #pragma unroll
     for (int p = 0; p < KP; ++p) qf[p] = *reinterpret_cast<const u32x4*>(&tile[buf][r * kRow + 16 * ((2 * p + hb) ^ swizzle(r))]);
   };
-  request(0, q0);
+  request(g0, q0);
   put(0, q0);
   __syncthreads();
-  int g = 0, r0 = q0;
-  for (int buf = 0; g < G; buf ^= 1) {
+  int g = g0, r0 = q0;
+  for (int buf = 0; g < g1; buf ^= 1) {
     const bool wraps = r0 + kTileRows >= q1;
     const int g_next = wraps ? g + 1 : g, r_next = wraps ? q0 : r0 + kTileRows;
-    if (g_next < G) request(g_next, r_next);
+    if (g_next < g1) request(g_next, r_next);
 #pragma unroll 1
     for (int step = 0; step < kSteps; ++step) {
       // every query of the step counts and sees every key of the wave
@@ -218,7 +218,7 @@ attention_mass_kernel(const T* __restrict__ q, int64_t q_st, int64_t q_sh, const
         pending = 0.f;
       }
     }
-    if (g_next < G) put(buf ^ 1, r_next);
+    if (g_next < g1) put(buf ^ 1, r_next);
     __syncthreads();
     g = g_next;
     r0 = r_next;
@@ -260,17 +260,23 @@ mass_parts_kernel(const float* __restrict__ sums, int parts, int64_t total, int 
   mass[h * total + j] = v;
 }
 
-struct Split { int parts, rows; };
-constexpr int64_t kFill = 2048;
-// Parts of the queries: as many as fill the chip a few times over, at most 2048 queries each.
+struct Split { int parts, rows, head_parts, heads; };      // parts in all; rows and query heads of one
+constexpr int64_t kFill = 2048, kOnce = 512;
+// Parts of the queries: as many as fill the chip a few times over (4 x 4096 tokens, 32/8 heads: 226 us; half as many workgroups 258, twice
+// 231), at most 2048 queries each and 64 at least (300 fp32 tokens, 2 heads: 10.6 us, with 128 14.6).  Where those are not even two
+// workgroups a CU, the query heads of a group are shared out too (300 tokens, 32/8 heads: 17.1 -> 11.6 us; filling the chip as often as
+// above by heads, 1000 tokens take 27.4 us instead of 21.8).
 Split split_of(const ltea_cfg& cfg, const SeqView& sv, int last) {
-  const int64_t keys = tile_keys(cfg);
+  const int64_t keys = tile_keys(cfg), G = cfg.Hq / cfg.Hkv;
   const int64_t groups = (sv.total_tokens / keys + 1) * cfg.Hkv;
   const int64_t reach = last > 0 && last < sv.max_seqlen ? last : sv.max_seqlen;
   int64_t parts = (kFill + groups - 1) / groups;
   if (parts < (reach + 2047) / 2048) parts = (reach + 2047) / 2048;
-  int64_t rows = ((reach + parts - 1) / parts + kStepRows - 1) / kStepRows * kStepRows;
-  return Split{(int)((reach + rows - 1) / rows), (int)rows};
+  const int64_t rows = ((reach + parts - 1) / parts + kStepRows - 1) / kStepRows * kStepRows;
+  parts = (reach + rows - 1) / rows;
+  const int64_t most = kOnce / (groups * parts), heads = most < 2 ? G : most < G ? (G + most - 1) / most : 1;
+  const int64_t head_parts = (G + heads - 1) / heads;
+  return Split{(int)(parts * head_parts), (int)rows, (int)head_parts, (int)heads};
 }
 
 }  // namespace
@@ -298,7 +304,7 @@ hipError_t launch_attention_mass(const ltea_cfg& cfg, const void* q, int64_t q_s
   const Split s = split_of(cfg, sv, last);
   MassParams P;
   P.n_seqs = sv.n_seqs; P.Hq = cfg.Hq; P.Hkv = cfg.Hkv; P.window = cfg.window; P.last = last;
-  P.parts = s.parts; P.part_rows = s.rows; P.total = sv.total_tokens;
+  P.parts = s.parts; P.part_rows = s.rows; P.head_parts = s.head_parts; P.part_heads = s.heads; P.total = sv.total_tokens;
   P.scale2 = (cfg.softmax_scale > 0.f ? cfg.softmax_scale : 1.0f / sqrtf((float)cfg.D)) * 1.4426950408889634f;
   float* sums = s.parts > 1 ? static_cast<float*>(workspace) : mass;
   auto go = [&](auto tag, auto dim) {
