@@ -87,3 +87,18 @@ def test_prompts_of_no_tokens_start_a_cache():
     assert B.ltea_attention_mass(cfg, q, k, cu, 0, torch.empty((4, 0), device="cuda")).shape == (2, 0)
     for step in range(2):
         run_and_check(cfg, cache, None, True, 540 + step, "bf16")
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,dtype", [(5, 1, 64, "bf16"), (17, 1, 128, "bf16"), (60, 4, 64, "bf16"), (7, 1, 64, "f32")])
+@pytest.mark.parametrize("n,last", [(1, 0), (70, 0), (300, 0), (900, 100)])
+def test_weights_of_groups_in_parts(Hq, Hkv, D, dtype, n, last):
+    """Short prompts: the heads of a group in parts that need not be equal."""
+    rng = np.random.default_rng(36)
+    q, k = [torch.from_numpy(rng.standard_normal((n, h, D))).to(dtype=B.torch_dtype(dtype), device="cuda") for h in (Hq, Hkv)]
+    x, y = f64(q), f64(k)
+    lse = ko.causal_lse(x, y, n, D ** -0.5).astype(np.float32)
+    want = ko.attention_mass(x, y, lse.astype(np.float64), n, last, D ** -0.5)
+    cfg = B.make_cfg(Hq, Hkv, D, n, 0, 0, 0.0, 0.0, dtype)
+    cu = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    got = f64(B.ltea_attention_mass(cfg, q, k, cu, n, torch.from_numpy(lse).cuda(), last=last))
+    assert (np.abs(got - want) <= 2.0 ** -15 * want + 1e-30).all()           # as above
