@@ -296,7 +296,8 @@ template <typename T, int D, int GT> struct Running {
     for (int n = 0; n < D / 16; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   // x: q . k, -inf where the row does not count; scale2: softmax scale in log2 units (positive)
-  template <typename R> __device__ __forceinline__ void add(const R& rows, const float (&x)[8], float scale2, bool second_term) {
+  // take: 1, or 0: every term is the leading one (what is finite then is not wanted)
+  template <typename R> __device__ __forceinline__ void add(const R& rows, const float (&x)[8], float scale2, bool second_term, float take_lead) {
     float top = x[0];
 #pragma unroll
     for (int u = 1; u < 8; ++u) top = fmaxf(top, x[u]);
@@ -321,7 +322,7 @@ template <typename T, int D, int GT> struct Running {
       add_values(rows, p, o);
     } else {
       u32x4 first, rest;               // the bf16 values, two to a word, and those of what they leave
-      const float take = kTermColumns && !second_term ? 0.f : 1.f;
+      const float take = kTermColumns ? second_term ? 1.f : 0.f : take_lead;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const bf16x2 hi = {(bf16_t)p[2 * w], (bf16_t)p[2 * w + 1]};
@@ -604,9 +605,10 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
   __shared__ float red_m[W][16], red_l[W][16];
   __shared__ Entry red_e[W];
   __shared__ float ve_lds[D];
+  __shared__ int pass_again;
   __shared__ __align__(16) u32x4 q_lds[sizeof(T) == 2 ? (PK ? 2 : 1) * kQ * kWave : 1];      // bf16: a pass's queries as B operands, [rows, packed rows][piece][lane]
   __shared__ __align__(16) T rows_lds[4][D];          // keys of the incoming and of the leaving token, the latter's value, the former's
-  static_assert(sizeof(red_m) + sizeof(red_l) + sizeof(red_e) + sizeof(ve_lds) + sizeof(q_lds) + sizeof(rows_lds) + kKeptLds <= 64 * 1024, "LDS");
+  static_assert(sizeof(red_m) + sizeof(red_l) + sizeof(red_e) + sizeof(ve_lds) + sizeof(pass_again) + sizeof(q_lds) + sizeof(rows_lds) + kKeptLds <= 64 * 1024, "LDS");
   const int tid = threadIdx.x, lane = tid & (kWave - 1), c = lane & 15, kg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n = WHOLE ? 1 : P.L.nsplit, G = P.L.G;
@@ -736,6 +738,13 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
   Running<T, D, GT> run;
   T q_ahead[2][D / 64];
   FirstRows first;
+  // An infinite value times the lower terms of a probability, zero or of either sign, is not the infinity that the probability itself
+  // makes of it: an output that is not finite is what the leading terms give.  Where terms are columns, the leading one is at hand; else
+  // a pass with such an output is taken again, all its terms the leading one, for those outputs.
+  constexpr bool kTermPasses = Running<T, D, GT>::kTerms > 1;
+  float take = 1.f;
+  uint32_t not_finite = 0u;        // of this thread's outputs of the pass
+  if (kTermPasses && tid == 0) pass_again = 0;
   for (int g0 = 0;;) {
     run.reset();
     const bool mine = g0 + col < G;
@@ -801,7 +810,7 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
         next_k(blk + W, blk + W < end);
         if (partial) rows.clear(dead_rows(n_live, special));
         finish_scores(x, n_live, special, at0 + 32 * blk, kept, partial);
-        run.add(rows, x, P.scale2, second);
+        run.add(rows, x, P.scale2, second, take);
         next_v(blk + W, blk + W < end);
       }
     };
@@ -836,7 +845,7 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
             scores_of(K[i], 1, x);
             if (partial) K[i].clear(dead_rows(n_live, special));
             finish_scores(x, n_live, special, at_kept + 32 * blk, true, partial);
-            run.add(K[i], x, P.scale2, second);
+            run.add(K[i], x, P.scale2, second, take);
           }
           K[i].load(blocks + (int64_t)(blk + kDepth * W) * PackGeo<D>::kBlock, blk + kDepth * W < kept_end);
         }
@@ -874,13 +883,17 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         float o = run.o[x][r];
-        if constexpr (Running<T, D, GT>::kTermColumns)          // the other term's column: eight lanes on, in the row of 16
-          o += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(o), 0x128, 0xf, 0xf, false));
+        if constexpr (Running<T, D, GT>::kTermColumns) {        // the other term's column: eight lanes on, in the row of 16
+          const float rest = __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(o), 0x128, 0xf, 0xf, false));
+          o = fabsf(o) < INFINITY ? o + rest : o;
+        }
         if (mine && !second) red_o[(wave * heads_at_once + col) * kRow + (D / 16) * (4 * kg + r) + x] = o;      // output tile x, row 4 kg + r
       }
     __syncthreads();
     const int heads = G - g0 < GT ? G - g0 : GT;
-    for (int i = tid; i < heads * D; i += NT) {
+    uint32_t bit = 1u;               // at most 16 heads * D / NT = 8 outputs
+    for (int i = tid; i < heads * D; i += NT, bit <<= 1) {
+      if (kTermPasses && take == 0.f && !(not_finite & bit)) continue;
       const int gl = i / D, d = i - gl * D, g = g0 + gl;
       float M = -INFINITY, L = 0.f, A = 0.f;
 #pragma unroll
@@ -909,10 +922,18 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
         if (d == 0) { r[0] = M; r[1] = L; }
         r[2 + d] = A;
       }
+      if (kTermPasses && take != 0.f && !(fabsf(A) < INFINITY)) not_finite |= bit;
     }
+    if (kTermPasses && take != 0.f && not_finite != 0u) pass_again = 1;
+    if (kTermPasses && take == 0.f && tid == 0) pass_again = 0;
     __syncthreads();
-    g0 += GT;
-    if (g0 >= G) break;
+    const bool again = kTermPasses && take != 0.f && pass_again != 0;
+    take = again ? 0.f : 1.f;
+    if (!again) {
+      not_finite = 0u;
+      g0 += GT;
+      if (g0 >= G) break;
+    }
     request_queries(g0);
     load_ring_k(first_ring, first_ring < ring_end);          // (here: requested rows are not held through the loops above)
     load_ring_v(first_ring, first_ring < ring_end);
