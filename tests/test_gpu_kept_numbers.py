@@ -1,4 +1,4 @@
-"""Infinite values in the steps over kept entries, with bounds that stay finite whatever the rows hold."""
+"""Infinite values and rows that go in the steps over kept entries, with bounds that stay finite whatever the rows hold."""
 import numpy as np
 import pytest
 import torch
@@ -82,3 +82,25 @@ def test_infinite_values(form, D, G, packed):
             check(got, ref, rows, (b, h))
             seen += int(np.isinf(ref).any()) + int(np.isfinite(ref).any())
     assert seen > 0
+
+
+@pytest.mark.parametrize("packed", [False, True], ids=["rows", "packed"])
+@pytest.mark.parametrize("G", [2, 7])
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_that_go_hold_anything(D, G, packed):
+    """The output next to a row that is dropped, and to one that is displaced, is finite and right to the same bound."""
+    cfg = B.make_cfg(2 * G, 2, D, 40, 50, 0, 0.0, 0.0, "bf16")
+    cache = make_state(cfg, [200, 200, 200], [50, 50, 50], 17)
+    slot = 200 % 40
+    cache.win_score[0, :, slot] = 0.0                                  # dropped by the threshold
+    cache.k_win[0, :, slot], cache.v_win[0, :, slot] = INF, float("nan")
+    cache.win_score[1, :, slot] = 5.0                                  # displaces the lowest
+    cache.ret_score[1, :, 9] = 1e-6
+    cache.k_ret[1, :, 9], cache.v_ret[1, :, 9] = float("nan"), INF
+    cache.win_score[2, :, slot] = 5.0
+    cache.ret_score[2, :, 33] = 1e-6
+    cache.k_ret[2, :, 33], cache.v_ret[2, :, 33] = -INF, -INF
+    pk = B.ltea_kept_pack(cfg, cache) if packed else None
+    for b, h, got, ref, rows, st in one_step(cfg, cache, pk, True, 600, 1):
+        assert st["dst"] == (None, 9, 33)[b] and np.isfinite(rows).all() and np.isfinite(ref).all()
+        check(got, ref, rows, (b, h))
