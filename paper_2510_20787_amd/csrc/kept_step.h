@@ -22,9 +22,9 @@
 //   O^T[d, head] += V^T . P^T      V in registers, eight rows of a few channels per lane, brought into the A operand's order by
 //                                  byte permutes; P from S^T's accumulators without leaving the lane: tile row m = 4 kg + r of
 //                                  tile j is row 8 kg + 4 j + r, so a lane's eight probabilities are eight consecutive rows
-// P is a bf16 value and the bf16 rounding of what that leaves out: 16 bits, against the 8 of the output.  For up to eight query
-// heads the two are columns of one matrix instruction, else two instructions.  fp32 storage: v_mfma_f32_16x16x4_f32 for both
-// products, P in 32 bits.
+// P is the exact sum of three bf16 terms, so that it keeps its 32 bits beside the 8 of the values.  For up to five query heads the terms
+// are columns of one matrix instruction (column 5 * term + head; every lane works out its head's probability and keeps its column's
+// term), else three instructions.  fp32 storage: v_mfma_f32_16x16x4_f32 for both products, P in 32 bits.
 #pragma once
 #include "fp4_rows.h"
 #include "kept_run.h"
@@ -238,7 +238,7 @@ template <int N> __device__ __forceinline__ bf16x8 rows_of_channel(const uint32_
   return __builtin_bit_cast(bf16x8, a);
 }
 
-// o[n] += V^T of channel n . P^T.  kTerms: P as one operand (columns hold the terms) or as two.
+// o[n] += V^T of channel n . P^T.  kTerms: P as one operand (columns hold the terms) or as three.
 template <int D, int kTerms> __device__ __forceinline__ void add_values(const StoredRows<bf16_t, D>& R, const bf16x8 (&p)[kTerms], f32x4 (&o)[D / 16]) {
 #pragma unroll
   for (int n = 0; n < D / 16; ++n) {
@@ -284,8 +284,8 @@ template <int D> __device__ __forceinline__ void add_values(const PackedRows<D>&
 
 // ---- a wave's running softmax -------------------------------------------------------------------------------------------------
 template <typename T, int D, int GT> struct Running {
-  static constexpr bool kTermColumns = sizeof(T) == 2 && GT == 8;
-  static constexpr int kTerms = sizeof(T) == 2 && GT == 16 ? 2 : 1;
+  static constexpr bool kTermColumns = sizeof(T) == 2 && GT == 5;
+  static constexpr int kTerms = sizeof(T) == 2 && GT == 16 ? 3 : 1;
   float m = -INFINITY, l = 0.f;       // of the lane's column; l: of the lane's rows
   f32x4 o[D / 16];
 
@@ -296,8 +296,8 @@ template <typename T, int D, int GT> struct Running {
     for (int n = 0; n < D / 16; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   // x: q . k, -inf where the row does not count; scale2: softmax scale in log2 units (positive)
-  // take: 1, or 0: every term is the leading one (what is finite then is not wanted)
-  template <typename R> __device__ __forceinline__ void add(const R& rows, const float (&x)[8], float scale2, bool second_term, float take_lead) {
+  // term: of the lane's column; take: 1, or 0: every term is the leading one (what is finite then is not wanted)
+  template <typename R> __device__ __forceinline__ void add(const R& rows, const float (&x)[8], float scale2, int term, float take) {
     float top = x[0];
 #pragma unroll
     for (int u = 1; u < 8; ++u) top = fmaxf(top, x[u]);
@@ -321,20 +321,25 @@ template <typename T, int D, int GT> struct Running {
     if constexpr (sizeof(T) == 4) {
       add_values(rows, p, o);
     } else {
-      u32x4 first, rest;               // the bf16 values, two to a word, and those of what they leave
-      const float take = kTermColumns ? second_term ? 1.f : 0.f : take_lead;
+      // p = top + middle + rest, exactly, cut to 8 bits each.  Columns: a lane's term is what the ones above it leave, cut in turn.
+      auto cut = [](float y) { return __uint_as_float(__float_as_uint(y) & 0xFFFF0000u); };
+      const float from_second = kTermColumns ? term > 0 ? 1.f : 0.f : take, from_third = kTermColumns ? term > 1 ? 1.f : 0.f : take;
+      u32x4 words[kTerms];
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const bf16x2 hi = {(bf16_t)p[2 * w], (bf16_t)p[2 * w + 1]};
-        first[w] = __builtin_bit_cast(uint32_t, hi);
-        const float lo0 = fmaf(-take, __uint_as_float(first[w] << 16), p[2 * w]);
-        const float lo1 = fmaf(-take, __uint_as_float(first[w] & 0xFFFF0000u), p[2 * w + 1]);
-        const bf16x2 lo = {(bf16_t)lo0, (bf16_t)lo1};
-        rest[w] = __builtin_bit_cast(uint32_t, lo);
+        float y[2] = {p[2 * w], p[2 * w + 1]};
+        auto pair = [&]() { return __builtin_amdgcn_perm(__float_as_uint(y[1]), __float_as_uint(y[0]), 0x07060302u); };      // upper halves
+        if constexpr (!kTermColumns) words[0][w] = pair();
+#pragma unroll
+        for (int e = 0; e < 2; ++e) y[e] = fmaf(-from_second, cut(y[e]), y[e]);
+        if constexpr (!kTermColumns) words[1][w] = pair();
+#pragma unroll
+        for (int e = 0; e < 2; ++e) y[e] = fmaf(-from_third, cut(y[e]), y[e]);
+        words[kTerms - 1][w] = pair();
       }
       bf16x8 t[kTerms];
-      t[0] = __builtin_bit_cast(bf16x8, kTermColumns ? rest : first);
-      t[kTerms - 1] = __builtin_bit_cast(bf16x8, rest);
+#pragma unroll
+      for (int z = 0; z < kTerms; ++z) t[z] = __builtin_bit_cast(bf16x8, words[z]);
       add_values<D, kTerms>(rows, t, o);
     }
   }
@@ -597,7 +602,9 @@ __global__ void __launch_bounds__(W * kWave, sizeof(T) == 4 || D == 128 ? 2 : PK
 kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __restrict__ k_new, const T* __restrict__ v_new,
                  T* __restrict__ out) {
   using S = StoredRows<T, D>;
-  constexpr int NT = W * kWave, kRow = D + 4, kDepth = sizeof(T) == 4 ? 1 : 3;      // kDepth: blocks of packed rows in flight per wave
+  constexpr int NT = W * kWave, kRow = D + 4, kDepth = sizeof(T) == 4 ? 1 : GT == 16 ? 2 : 3;
+  // kDepth: blocks of packed rows in flight per wave (GT = 16: three spill, 256 heads of 512 + 4096 rows, eight query heads each, D = 128: 50.8
+  // us, two 46.4)
   constexpr int kQ = sizeof(T) == 4 ? D / 4 : D / 32;
   // [W][heads of a pass][kRow] outputs of the waves, [2][G] scores of the incoming and the leaving token, [G] top, [G] inv,
   // [G] scores of the lowest entry, then the scores of all slots [G][slots]
@@ -634,8 +641,8 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
 
   // Requested before anything is known: the scalar words (scalar loads do not wait for rows requested earlier, vector loads return in
   // order), the queries, the first keys of the share, and last the wave's first rows, whatever they hold.
-  const int col = Running<T, D, GT>::kTermColumns ? c & 7 : c;
-  const bool second = Running<T, D, GT>::kTermColumns && c >= 8;
+  // this lane's column: a head of the pass and the term of its probabilities (of the last column: none)
+  const int col = Running<T, D, GT>::kTermColumns ? c % 5 : c, term = Running<T, D, GT>::kTermColumns ? c / 5 : 0;
   constexpr int kSets = PK ? 2 : 1, kMine = (kSets * kQ + W - 1) / W;      // bf16: pieces of the queries that a wave brings into LDS
   u32x4 q_piece[sizeof(T) == 2 ? kMine : 1];
   auto query_row = [&](int g0) { return q + ((int64_t)b * P.Hq + h * G + (g0 + col < G ? g0 + col : 0)) * D; };
@@ -653,7 +660,7 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
       for (int i = 0; i < kMine; ++i)
-        if (wave + i * W < kSets * kQ) q_lds[(wave + i * W) * kWave + lane] = g0 + col < G ? q_piece[i] : u32x4{0u, 0u, 0u, 0u};
+        if (wave + i * W < kSets * kQ) q_lds[(wave + i * W) * kWave + lane] = term < 3 && g0 + col < G ? q_piece[i] : u32x4{0u, 0u, 0u, 0u};
     }
   };
   request_queries(0);
@@ -749,7 +756,7 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
     run.reset();
     const bool mine = g0 + col < G;
     const T* qr = query_row(g0);
-    const bool writes = P.mass && mine && !second;
+    const bool writes = P.mass && mine && term == 0;
     float* my_scores = rest + (int64_t)(g0 + col) * P.L.slots + 8 * kg;                               // in LDS
     const uint32_t my_offset = writes ? (uint32_t)(((g0 + col) * P.L.slots + 8 * kg) * 4) : 1u << 31;      // or in the workspace
     float q_reg[sizeof(T) == 4 ? kQ : 1];      // fp32
@@ -772,7 +779,7 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
           const int r = r0 + u;
-          if (kept && r == special && mine && !second) low_x[g0 + col] = x[u];
+          if (kept && r == special && mine && term == 0) low_x[g0 + col] = x[u];
           x[u] = r < n_live && r != special ? x[u] : -INFINITY;
         }
       }
@@ -810,7 +817,7 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
         next_k(blk + W, blk + W < end);
         if (partial) rows.clear(dead_rows(n_live, special));
         finish_scores(x, n_live, special, at0 + 32 * blk, kept, partial);
-        run.add(rows, x, P.scale2, second, take);
+        run.add(rows, x, P.scale2, term, take);
         next_v(blk + W, blk + W < end);
       }
     };
@@ -845,7 +852,7 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
             scores_of(K[i], 1, x);
             if (partial) K[i].clear(dead_rows(n_live, special));
             finish_scores(x, n_live, special, at_kept + 32 * blk, true, partial);
-            run.add(K[i], x, P.scale2, second, take);
+            run.add(K[i], x, P.scale2, term, take);
           }
           K[i].load(blocks + (int64_t)(blk + kDepth * W) * PackGeo<D>::kBlock, blk + kDepth * W < kept_end);
         }
@@ -883,11 +890,12 @@ kept_step_kernel(CacheDev C, KeptParams P, const T* __restrict__ q, const T* __r
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         float o = run.o[x][r];
-        if constexpr (Running<T, D, GT>::kTermColumns) {        // the other term's column: eight lanes on, in the row of 16
-          const float rest = __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(o), 0x128, 0xf, 0xf, false));
-          o = fabsf(o) < INFINITY ? o + rest : o;
+        if constexpr (Running<T, D, GT>::kTermColumns) {        // the other terms' columns: five and ten lanes on, in the row of 16
+          const float middle = __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(o), 0x12B, 0xf, 0xf, false));
+          const float rest = __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(o), 0x126, 0xf, 0xf, false));
+          o = fabsf(o) < INFINITY ? o + (middle + rest) : o;
         }
-        if (mine && !second) red_o[(wave * heads_at_once + col) * kRow + (D / 16) * (4 * kg + r) + x] = o;      // output tile x, row 4 kg + r
+        if (mine && term == 0) red_o[(wave * heads_at_once + col) * kRow + (D / 16) * (4 * kg + r) + x] = o;      // output tile x, row 4 kg + r
       }
     __syncthreads();
     const int heads = G - g0 < GT ? G - g0 : GT;
@@ -1093,14 +1101,13 @@ hipError_t kept_run(const ltea_cfg& cfg, const KeptInputs& in, const ltea_cache&
   auto go = [&](auto pk, auto gt) {
     const integral_constant<int, kStepWaves> four;
     if (!whole) return launch(pk, gt, std::false_type{}, four);
-    if constexpr (decltype(gt)::value * D <= 1024) {          // (the outputs of eight waves: 34 KB of LDS)
-      if (split.waves == 8) return launch(pk, gt, true_type{}, integral_constant<int, 8>{});
-    }
+    // (the outputs of eight waves: 34 KB of LDS)
+    if (split.waves == 8 && (G < decltype(gt)::value ? G : decltype(gt)::value) * D <= 1024) return launch(pk, gt, true_type{}, integral_constant<int, 8>{});
     return launch(pk, gt, true_type{}, four);
   };
   auto by_heads = [&](auto pk) {
     if constexpr (sizeof(T) == 2) {
-      if (G <= 8) return go(pk, integral_constant<int, 8>{});
+      if (G <= 5) return go(pk, integral_constant<int, 5>{});
     }
     return go(pk, integral_constant<int, 16>{});
   };

@@ -104,3 +104,48 @@ def test_rows_that_go_hold_anything(D, G, packed):
     for b, h, got, ref, rows, st in one_step(cfg, cache, pk, True, 600, 1):
         assert st["dst"] == (None, 9, 33)[b] and np.isfinite(rows).all() and np.isfinite(ref).all()
         check(got, ref, rows, (b, h))
+
+
+@pytest.mark.parametrize("segment", ["ring", "kept"])
+@pytest.mark.parametrize("G", [1, 4, 5, 6, 8, 16, 17])
+@pytest.mark.parametrize("D", [64, 128])
+def test_probabilities_keep_32_bits(D, G, segment):
+    """Three rows whose values cancel: two correct, to 8 bits each, what the first leaves, so that the output is below 2^-14 of the terms and
+    its own rounding below 2^-22 of them.  What shows is the probabilities' precision.
+
+    A score is the product of two bf16 values, exact.  Its exponent is a product with a rounded scale minus a rounded reference, of size
+    up to 3: three roundings of 3 * 2^-24, 2^-21.3 of a probability by ln 2, and the exponential's and the sum's own, 2^-22 together.
+    Bar 2^-20 of the terms; probabilities cut to 16 bits are off by up to 2^-17 of theirs."""
+    rng = np.random.default_rng(8 * D + G)
+    bf = lambda x: torch.as_tensor(np.asarray(x), dtype=torch.float64).to(torch.bfloat16).double().numpy()
+    cfg = B.make_cfg(G, 1, D, 40, 40, 0, 0.0, 0.25, "bf16")
+    kept = segment == "kept"
+    cache = make_state(cfg, [43 if kept else 3], [3 if kept else 0], 44)
+    # the query looks at channel 0: scores of a quarter of the product; the incoming token far below
+    heads = bf(rng.uniform(1.0, 1.5, G))
+    q, k = np.zeros((1, G, D)), np.zeros((1, 1, D))
+    q[0, :, 0], k[0, 0, 0] = heads, -400.0
+    keys = bf(rng.uniform(-4.0, 0.0, 3))
+    x = 0.25 * heads[:, None] * keys[None]
+    p = np.exp(x)                                                             # [G, 3]
+    v = np.zeros((3, D))
+    v[0] = bf(rng.standard_normal(D))
+    for i in (1, 2):                                                          # channel d cancels for query head d % G
+        for d in range(D):
+            v[i, d] = bf(-(p[d % G, :i] @ v[:i, d]) / p[d % G, i])
+    put = lambda a, dt=torch.bfloat16: torch.from_numpy(np.ascontiguousarray(a)).to(dtype=dt, device="cuda")
+    if kept:                                                                  # a ring of rows that count nothing beside them
+        cache.k_win[...] = 0.0
+        cache.k_win[..., 0] = -400.0
+        cache.v_win[...] = 0.0
+    to_k, to_v = (cache.k_ret, cache.v_ret) if kept else (cache.k_win, cache.v_win)
+    to_k[0, 0, :3] = 0.0
+    to_k[0, 0, :3, 0], to_v[0, 0, :3] = put(keys), put(v)
+    cache.win_score[...] = 0.0                                                # (what leaves is dropped)
+    got = f64(B.ltea_decode_step_mass(cfg, put(q), put(k), put(np.zeros((1, 1, D))), cache))[0]
+    total = p.sum(1, keepdims=True)
+    ref, terms = (p @ v) / total, (p @ np.abs(v)) / total
+    own = np.arange(D) % G == np.arange(G)[:, None]
+    assert (np.abs(ref[own]) <= 2.0 ** -14 * terms[own]).all()
+    err = np.abs(got - ref)
+    assert (err <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -20 * terms)[own].all(), float((err / terms)[own].max() * 2 ** 20)
