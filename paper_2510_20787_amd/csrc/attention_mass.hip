@@ -192,15 +192,13 @@ attention_mass_kernel(const T* __restrict__ q, int64_t q_st, int64_t q_sh, const
         }
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
-          const int i0 = r1 + 32 * half, i_q = i0 + c;
+          const int i0 = r1 + 32 * half;
           // no query, all queries before the wave's keys, or all keys out of their windows
           if (i0 >= q1 || i0 + 31 < my0 || i0 - (my0 + 32 * KB - 1) >= P.window) continue;
           u32x4 qf[KP];
           float l2;
           load_q(buf, 2 * step + half, qf, l2);
-          if (!(l2 < INFINITY))
-#pragma unroll
-            for (int p = 0; p < KP; ++p) qf[p] = u32x4{0u, 0u, 0u, 0u};
+          const int i_q = l2 < INFINITY ? i0 + c : -1;      // a query that does not count sees nothing, whatever its row and the keys hold
 #pragma unroll
           for (int x = 0; x < KB; ++x) {
             const int j0 = my0 + 32 * x;
