@@ -14,7 +14,9 @@
 //
 // A workgroup takes 4 waves x KB blocks of 32 keys of one (sequence, KV head) and a part of the queries that can see them, all
 // query heads of the group.  Parts meet in a second launch, in their order: same bits every time, and sums of at most 2048 queries
-// per head in one register chain.
+// per head in one register chain.  Only parts that reach a key write sums for it; where a window keeps the others away, parts are counted
+// from the first that does.  Prompts of more parts than a launch takes (16, or as many as fill the chip) take several pairs of launches,
+// so that the sums need no more room than that.
 #include "ltea_common.h"
 #include "ltea_kernels.h"
 #include "mfma_tiles.h"
@@ -35,19 +37,24 @@ int64_t tile_keys(const ltea_cfg& cfg) {
 }
 
 struct MassParams {
-  int n_seqs, tiles_upper, Hq, Hkv, window, last, parts, part_rows, head_parts, part_heads, units;
+  int n_seqs, tiles_upper, Hq, Hkv, window, last, part_rows, head_parts, part_heads, units;
+  int slot0, slots;              // of this launch
+  bool relative, whole;          // slots count from a key's first part; sums are the weights: one part in all
   int64_t total;
   float scale2;
 };
 
-// Queries of part `part` of a sequence of n tokens that can see a key of [lo, hi) and count.
-__device__ __forceinline__ void queries_of(const MassParams& P, int part, int n, int lo, int hi, int& q0, int& q1) {
-  const int first = P.last > 0 && n > P.last ? n - P.last : 0;
-  const int64_t from = first + (int64_t)part * P.part_rows, reach = (int64_t)hi - 1 + P.window;
-  const int64_t to = from + P.part_rows < reach ? from + P.part_rows : reach;
-  q0 = (int)(from < lo ? lo / kStepRows * kStepRows > from ? lo / kStepRows * kStepRows : from : from < n ? from : n);
-  q1 = (int)(to < n ? to : n);
-}
+// Of a sequence of n tokens, the counting queries [first, n) lie in parts of part_rows.  Slot 0 begins at query `from` for the keys
+// [lo, hi), which queries before `end` see.
+struct Slots {
+  uint32_t from, end;
+  __device__ __forceinline__ Slots(const MassParams& P, int n, int lo, int hi) {
+    const int first = P.last > 0 && n > P.last ? n - P.last : 0;
+    const uint32_t reach = (uint32_t)hi - 1u + (uint32_t)P.window, rows = (uint32_t)P.part_rows;
+    from = (uint32_t)first + (P.relative && lo > first ? (uint32_t)(lo - first) / rows * rows : 0u);
+    end = reach < (uint32_t)n ? reach : (uint32_t)n;
+  }
+};
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 2)
@@ -66,19 +73,20 @@ attention_mass_kernel(const T* __restrict__ q, int64_t q_st, int64_t q_sh, const
   // the most keys see, first.
   const int unit = (int)(blockIdx.x % 8 + blockIdx.x / 8 / P.tiles_upper * 8), flat = (int)(blockIdx.x / 8 % P.tiles_upper);
   if (unit >= P.units) return;
-  const int part = P.parts - 1 - unit / P.Hkv, h = unit % P.Hkv;
+  const int of_launch = P.slots * P.head_parts - 1 - unit / P.Hkv, h = unit % P.Hkv;
   int seq, tile_i, lo, n;
   if (!locate_tile(cu, P.n_seqs, kKeys, flat, seq, tile_i, lo, n)) return;
   const int key0 = tile_i * kKeys, key1 = key0 + kKeys < n ? key0 + kKeys : n;
-  int q0, q1;
-  queries_of(P, part / P.head_parts, n, key0, key1, q0, q1);
-  const int G = P.Hq / P.Hkv, g0 = part % P.head_parts * P.part_heads, g1 = g0 + P.part_heads < G ? g0 + P.part_heads : G;
-
-  float* to = sums + ((int64_t)part * P.Hkv + h) * P.total + lo;
-  if (q1 <= q0) {
-    for (int j = key0 + tid; j < key1; j += kThreads) to[j] = 0.f;
+  float* to = sums + ((int64_t)of_launch * P.Hkv + h) * P.total + lo;
+  const Slots slots(P, n, key0, key1);
+  const uint32_t from_q = slots.from + (uint32_t)(P.slot0 + of_launch / P.head_parts) * (uint32_t)P.part_rows, to_q = from_q + (uint32_t)P.part_rows;
+  const int q0 = from_q > (uint32_t)key0 ? (int)from_q : key0, q1 = to_q < slots.end ? (int)to_q : (int)slots.end;
+  if (from_q >= slots.end || q1 <= q0) {
+    if (P.whole)
+      for (int j = key0 + tid; j < key1; j += kThreads) to[j] = 0.f;
     return;
   }
+  const int G = P.Hq / P.Hkv, g0 = of_launch % P.head_parts * P.part_heads, g1 = g0 + P.part_heads < G ? g0 + P.part_heads : G;
 
   // this wave's keys
   const int my0 = key0 + wave * 32 * KB;
@@ -245,55 +253,76 @@ attention_mass_kernel(const T* __restrict__ q, int64_t q_st, int64_t q_sh, const
   }
 }
 
-// Tokens that are in no sequence keep what they have.
-__global__ void __launch_bounds__(kThreads)
-mass_parts_kernel(const float* __restrict__ sums, int parts, int64_t total, int Hkv, int blocks, const int32_t* __restrict__ cu, int n_seqs,
-                  float* __restrict__ mass) {
-  const int h = blockIdx.x / blocks;
-  const int64_t j = (int64_t)(blockIdx.x - h * blocks) * kThreads + threadIdx.x;
-  if (j < cu[0] || j >= cu[n_seqs]) return;
-  float v = 0.f;
+// The sums of a launch's parts, in their order, join those of the launches before.  A workgroup per key tile of the first kernel.
+template <int kKeys>
+__global__ void __launch_bounds__(kKeys)
+mass_parts_kernel(const float* __restrict__ sums, const int32_t* __restrict__ cu, MassParams P, float* __restrict__ mass) {
+  const int h = blockIdx.x / P.tiles_upper, flat = blockIdx.x - h * P.tiles_upper;
+  int seq, tile_i, lo, n;
+  if (!locate_tile(cu, P.n_seqs, kKeys, flat, seq, tile_i, lo, n)) return;
+  const int key0 = tile_i * kKeys, key1 = key0 + kKeys < n ? key0 + kKeys : n, j = key0 + threadIdx.x;
+  if (j >= key1) return;
+  float* to = mass + h * P.total + lo + j;
+  const float* from = sums + h * P.total + lo + j;
+  float v = P.slot0 == 0 ? 0.f : *to;
+  const Slots slots(P, n, key0, key1);
+  const uint32_t rows = (uint32_t)P.part_rows;
+  uint32_t q = slots.from + (uint32_t)P.slot0 * rows;
 #pragma unroll 4
-  for (int p = 0; p < parts; ++p) v += sums[((int64_t)p * Hkv + h) * total + j];
-  mass[h * total + j] = v;
+  for (int u = 0, hp = 0; u < P.slots * P.head_parts; ++u) {
+    const float x = from[(int64_t)u * P.Hkv * P.total];      // (of a part that does not reach: anything)
+    if (q < slots.end && q + rows > (uint32_t)key0) v += x;
+    if (++hp == P.head_parts) { hp = 0; q += rows; }
+  }
+  *to = v;
 }
 
-struct Split { int parts, rows, head_parts, heads; };      // parts in all; rows and query heads of one
-constexpr int64_t kFill = 2048, kOnce = 512;
+struct Split { int slots, each, rows, head_parts, heads; bool relative; };      // parts that reach a key, and of one launch; rows and query heads of one
+constexpr int64_t kFill = 2048, kOnce = 512, kEach = 16;
 // Parts of the queries: as many as fill the chip a few times over (4 x 4096 tokens, 32/8 heads: 226 us; half as many workgroups 258, twice
 // 231), at most 2048 queries each and 64 at least (300 fp32 tokens, 2 heads: 10.6 us, with 128 14.6).  Where those are not even two
 // workgroups a CU, the query heads of a group are shared out too (300 tokens, 32/8 heads: 17.1 -> 11.6 us; filling the chip as often as
 // above by heads, 1000 tokens take 27.4 us instead of 21.8).
+// A launch takes 16 parts, or as many as fill the chip: sums of 64 bytes a token and KV head, whatever the length (131072 tokens, 8 heads,
+// D = 128: 17.95 ms in four pairs of launches, 17.87 in one with four times the room).  With a window only the parts that reach a key have a
+// slot (the same with a window of 2048: 0.82 ms, with a slot for every part 1.19).
 Split split_of(const ltea_cfg& cfg, const SeqView& sv, int last) {
   const int64_t keys = tile_keys(cfg), G = cfg.Hq / cfg.Hkv;
   const int64_t groups = (sv.total_tokens / keys + 1) * cfg.Hkv;
   const int64_t reach = last > 0 && last < sv.max_seqlen ? last : sv.max_seqlen;
-  int64_t parts = (kFill + groups - 1) / groups;
+  const int64_t fill = (kFill + groups - 1) / groups;
+  int64_t parts = fill;
   if (parts < (reach + 2047) / 2048) parts = (reach + 2047) / 2048;
   const int64_t rows = ((reach + parts - 1) / parts + kStepRows - 1) / kStepRows * kStepRows;
   parts = (reach + rows - 1) / rows;
   const int64_t most = kOnce / (groups * parts), heads = most < 2 ? G : most < G ? (G + most - 1) / most : 1;
   const int64_t head_parts = (G + heads - 1) / heads;
-  return Split{(int)(parts * head_parts), (int)rows, (int)head_parts, (int)heads};
+  // a key tile and its window: so many queries, which begin anywhere in a part
+  const int64_t seen = (cfg.window + keys - 1 + rows - 2) / rows + 1, slots = seen < parts ? seen : parts;
+  const int64_t each = fill > kEach ? fill : kEach;
+  return Split{(int)slots, (int)(slots < each ? slots : each), (int)rows, (int)head_parts, (int)heads, seen < parts};
 }
 
 }  // namespace
 
 size_t mass_workspace(const ltea_cfg& cfg, const SeqView& sv, int last) {
   const Split s = split_of(cfg, sv, last);
-  return s.parts > 1 ? (size_t)s.parts * cfg.Hkv * sv.total_tokens * sizeof(float) : 0;
+  const int64_t sums = (int64_t)s.each * s.head_parts;
+  return s.slots * s.head_parts > 1 ? (size_t)sums * cfg.Hkv * sv.total_tokens * sizeof(float) : 0;
 }
-// Of any call of up to so many tokens: a part for every 2048 queries of the longest sequence and one more, or as many as fill the chip.
+// Of any call of up to so many tokens: sums for every 2048 queries of the longest sequence and one more, but not more than a launch takes,
+// or as many as fill the chip.
 size_t mass_workspace_most(const ltea_cfg& cfg, int64_t total, int32_t max_seqlen) {
-  const size_t keys = tile_keys(cfg);
-  return (kFill * keys + (size_t)cfg.Hkv * total * (2 + (size_t)max_seqlen / 2048)) * sizeof(float);
+  const size_t keys = tile_keys(cfg), sums = 2 + (size_t)max_seqlen / 2048;
+  return (kFill * keys + (size_t)cfg.Hkv * total * (sums < kEach ? sums : kEach)) * sizeof(float);
 }
 
 // The grid and the offsets inside a tile of queries are 32-bit numbers.
 bool mass_supported(const ltea_cfg& cfg, const SeqView& sv, int64_t q_st, int last) {
   if (q_st * (cfg.dtype == LTEA_F32 ? 4 : 2) * 128 >= (int64_t)1 << 31) return false;
-  const int64_t keys = tile_keys(cfg);
-  return sv.total_tokens == 0 || (sv.total_tokens / keys + sv.n_seqs) * ((int64_t)cfg.Hkv * split_of(cfg, sv, last).parts + 7) <= INT32_MAX;
+  if (sv.total_tokens == 0) return true;
+  const Split s = split_of(cfg, sv, last);
+  return (sv.total_tokens / tile_keys(cfg) + sv.n_seqs) * ((int64_t)cfg.Hkv * s.each * s.head_parts + 7) <= INT32_MAX;
 }
 
 hipError_t launch_attention_mass(const ltea_cfg& cfg, const void* q, int64_t q_st, int64_t q_sh, const void* k, int64_t k_st, int64_t k_sh,
@@ -302,26 +331,28 @@ hipError_t launch_attention_mass(const ltea_cfg& cfg, const void* q, int64_t q_s
   const Split s = split_of(cfg, sv, last);
   MassParams P;
   P.n_seqs = sv.n_seqs; P.Hq = cfg.Hq; P.Hkv = cfg.Hkv; P.window = cfg.window; P.last = last;
-  P.parts = s.parts; P.part_rows = s.rows; P.head_parts = s.head_parts; P.part_heads = s.heads; P.total = sv.total_tokens;
+  P.part_rows = s.rows; P.head_parts = s.head_parts; P.part_heads = s.heads; P.total = sv.total_tokens;
+  P.relative = s.relative; P.whole = s.slots * s.head_parts == 1;
   P.scale2 = (cfg.softmax_scale > 0.f ? cfg.softmax_scale : 1.0f / sqrtf((float)cfg.D)) * 1.4426950408889634f;
-  float* sums = s.parts > 1 ? static_cast<float*>(workspace) : mass;
+  P.tiles_upper = (int)(sv.total_tokens / tile_keys(cfg) + sv.n_seqs);
+  float* sums = P.whole ? mass : static_cast<float*>(workspace);
   auto go = [&](auto tag, auto dim) {
     using T = decltype(tag);
-    constexpr int D = decltype(dim)::value;
-    P.tiles_upper = (int)(sv.total_tokens / kTileKeys<T, D> + sv.n_seqs);
-    P.units = cfg.Hkv * s.parts;
-    hipLaunchKernelGGL((attention_mass_kernel<T, D>), dim3((unsigned)((int64_t)P.tiles_upper * ((P.units + 7) / 8 * 8))), dim3(kThreads), 0,
-                       stream, static_cast<const T*>(q), q_st, q_sh, static_cast<const T*>(k), k_st, k_sh, sv.cu_seqlens, lse, P, sums);
-    return hipGetLastError();
+    constexpr int D = decltype(dim)::value, kKeys = kTileKeys<T, D>;
+    for (P.slot0 = 0; P.slot0 < s.slots; P.slot0 += s.each) {
+      P.slots = s.slots - P.slot0 < s.each ? s.slots - P.slot0 : s.each;
+      P.units = cfg.Hkv * P.slots * s.head_parts;
+      hipLaunchKernelGGL((attention_mass_kernel<T, D>), dim3((unsigned)((int64_t)P.tiles_upper * ((P.units + 7) / 8 * 8))), dim3(kThreads), 0,
+                         stream, static_cast<const T*>(q), q_st, q_sh, static_cast<const T*>(k), k_st, k_sh, sv.cu_seqlens, lse, P, sums);
+      hipError_t e = hipGetLastError();
+      if (e != hipSuccess || P.whole) return e;
+      hipLaunchKernelGGL(mass_parts_kernel<kKeys>, dim3((unsigned)(P.tiles_upper * cfg.Hkv)), dim3(kKeys), 0, stream, sums, sv.cu_seqlens, P, mass);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    return hipSuccess;
   };
-  const hipError_t e = cfg.dtype == LTEA_F32
-                           ? (cfg.D == 64 ? go(float{}, std::integral_constant<int, 64>{}) : go(float{}, std::integral_constant<int, 128>{}))
-                           : (cfg.D == 64 ? go(bf16_t{}, std::integral_constant<int, 64>{}) : go(bf16_t{}, std::integral_constant<int, 128>{}));
-  if (e != hipSuccess || s.parts == 1) return e;
-  const int blocks = (int)((sv.total_tokens + kThreads - 1) / kThreads);
-  hipLaunchKernelGGL(mass_parts_kernel, dim3((unsigned)(blocks * cfg.Hkv)), dim3(kThreads), 0, stream, sums, s.parts, sv.total_tokens, cfg.Hkv,
-                     blocks, sv.cu_seqlens, sv.n_seqs, mass);
-  return hipGetLastError();
+  if (cfg.dtype == LTEA_F32) return cfg.D == 64 ? go(float{}, std::integral_constant<int, 64>{}) : go(float{}, std::integral_constant<int, 128>{});
+  return cfg.D == 64 ? go(bf16_t{}, std::integral_constant<int, 64>{}) : go(bf16_t{}, std::integral_constant<int, 128>{});
 }
 
 }  // namespace ltea
