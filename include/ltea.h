@@ -331,7 +331,8 @@ int ltea_decode_step_lazy(const ltea_cfg *cfg, const void *q, const void *k, con
  * j <= i < j + window and i >= n - last (last <= 0: all queries) of exp(scale * q_i . k_j - lse[hq][i]).
  * lse: [Hq][total_tokens] fp32, the natural log of query i's softmax normaliser (ltea_train_forward writes it); a query
  * whose lse is not finite counts nothing.  mass: [Hkv][total_tokens] fp32.  q, k: views as in ltea_prefill.  Of the
- * config budget, sink and tau_logit are ignored.  Same bits every time. */
+ * config budget, sink and tau_logit are ignored.  Same bits every time.  LTEA_EUNSUPPORTED: query rows of 2^24 bytes and more apart, or
+ * (total_tokens / 256 + n_seqs) * (Hkv + 7) of 2^24 and more (fp32: total_tokens / 128). */
 size_t ltea_mass_workspace_bytes(const ltea_cfg *cfg, int32_t n_seqs, int64_t total_tokens, int32_t max_seqlen);
 int ltea_attention_mass(const ltea_cfg *cfg, const void *q, int64_t q_stride_tok, int64_t q_stride_head, const void *k,
                         int64_t k_stride_tok, int64_t k_stride_head, const int32_t *cu_seqlens, int32_t n_seqs,
@@ -370,7 +371,7 @@ int ltea_kept_unpack(const ltea_cfg *cfg, const void *packed, const ltea_cache *
  * the key of every ring and compact entry grows by the weight that q_t's softmax gives it (the incoming token starts
  * at zero; a weight that is not a number counts nothing), and n_scored = n_seen.  packed_or_null: the compact rows are
  * there (k_ret, v_ret may then be NULL); the evicted token is attended as it is kept.  LTEA_EUNSUPPORTED: more than 128
- * query heads per KV head, more than 2^24 (sequence, KV head) pairs, or 4 * (Hq / Hkv) * (window + budget) of 2^31 bytes and
+ * query heads per KV head, 2^24 (sequence, KV head) pairs and more, or 4 * (Hq / Hkv) * (window + budget) of 2^31 bytes and
  * more.  Concurrent calls on the same cache or the same workspace race. */
 size_t ltea_decode_kept_workspace_bytes(const ltea_cfg *cfg, int32_t n_seqs);
 int ltea_decode_step_mass(const ltea_cfg *cfg, const void *q, const void *k, const void *v, void *out,

@@ -283,7 +283,7 @@ constexpr int64_t kFill = 2048, kOnce = 512, kEach = 16;
 // 231), at most 2048 queries each and 64 at least (300 fp32 tokens, 2 heads: 10.6 us, with 128 14.6).  Where those are not even two
 // workgroups a CU, the query heads of a group are shared out too (300 tokens, 32/8 heads: 17.1 -> 11.6 us; filling the chip as often as
 // above by heads, 1000 tokens take 27.4 us instead of 21.8).
-// A launch takes 16 parts, or as many as fill the chip: sums of 64 bytes a token and KV head, whatever the length (131072 tokens, 8 heads,
+// A launch takes 16 parts, or as many as fill the chip, and no more than a grid holds: sums of 64 bytes a token and KV head, whatever the length (131072 tokens, 8 heads,
 // D = 128: 17.95 ms in four pairs of launches, 17.87 in one with four times the room).  With a window only the parts that reach a key have a
 // slot (the same with a window of 2048: 0.82 ms, with a slot for every part 1.19).
 Split split_of(const ltea_cfg& cfg, const SeqView& sv, int last) {
@@ -299,7 +299,10 @@ Split split_of(const ltea_cfg& cfg, const SeqView& sv, int last) {
   const int64_t head_parts = (G + heads - 1) / heads;
   // a key tile and its window: so many queries, which begin anywhere in a part
   const int64_t seen = (cfg.window + keys - 1 + rows - 2) / rows + 1, slots = seen < parts ? seen : parts;
-  const int64_t each = fill > kEach ? fill : kEach;
+  // (units of eight key heads and parts, see the kernel)
+  const int64_t room = (kMaxThreads / kThreads / (sv.total_tokens / keys + sv.n_seqs) - 7) / (cfg.Hkv * head_parts);
+  int64_t each = fill > kEach ? fill : kEach;
+  if (each > room) each = room > 1 ? room : 1;
   return Split{(int)slots, (int)(slots < each ? slots : each), (int)rows, (int)head_parts, (int)heads, seen < parts};
 }
 
@@ -317,12 +320,12 @@ size_t mass_workspace_most(const ltea_cfg& cfg, int64_t total, int32_t max_seqle
   return (kFill * keys + (size_t)cfg.Hkv * total * (sums < kEach ? sums : kEach)) * sizeof(float);
 }
 
-// The grid and the offsets inside a tile of queries are 32-bit numbers.
+// The threads of a launch and the offsets inside a tile of queries are 32-bit numbers.
 bool mass_supported(const ltea_cfg& cfg, const SeqView& sv, int64_t q_st, int last) {
   if (q_st * (cfg.dtype == LTEA_F32 ? 4 : 2) * 128 >= (int64_t)1 << 31) return false;
   if (sv.total_tokens == 0) return true;
   const Split s = split_of(cfg, sv, last);
-  return (sv.total_tokens / tile_keys(cfg) + sv.n_seqs) * ((int64_t)cfg.Hkv * s.each * s.head_parts + 7) <= INT32_MAX;
+  return (sv.total_tokens / tile_keys(cfg) + sv.n_seqs) * ((int64_t)cfg.Hkv * s.each * s.head_parts + 7) <= kMaxThreads / kThreads;
 }
 
 hipError_t launch_attention_mass(const ltea_cfg& cfg, const void* q, int64_t q_st, int64_t q_sh, const void* k, int64_t k_st, int64_t k_sh,

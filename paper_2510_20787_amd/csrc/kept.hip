@@ -77,9 +77,9 @@ template <typename T> struct Eight {
 template <typename T, int D>
 __global__ void __launch_bounds__(kPackThreads)
 kept_pack_kernel(const T* __restrict__ k_ret, const T* __restrict__ v_ret, const int32_t* __restrict__ ret_count, int budget,
-                 int n_blocks, uint8_t* __restrict__ packed) {
-  const int64_t head = blockIdx.x / n_blocks;
-  const int blk = (int)(blockIdx.x - head * n_blocks);
+                 int n_blocks, uint32_t first, uint8_t* __restrict__ packed) {
+  const int64_t head = (first + blockIdx.x) / (uint32_t)n_blocks;
+  const int blk = (int)(first + blockIdx.x - (uint32_t)head * (uint32_t)n_blocks);
   const int count = ret_count[head], left = (count < budget ? count : budget) - 32 * blk;
   if (left <= 0) return;
   uint8_t* out = packed + (head * n_blocks + blk) * (int64_t)PackGeo<D>::kBlock;
@@ -122,10 +122,10 @@ kept_pack_kernel(const T* __restrict__ k_ret, const T* __restrict__ v_ret, const
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kPackThreads)
-kept_unpack_kernel(const uint8_t* __restrict__ packed, const int32_t* __restrict__ ret_count, int budget, int n_blocks,
+kept_unpack_kernel(const uint8_t* __restrict__ packed, const int32_t* __restrict__ ret_count, int budget, int n_blocks, uint32_t first,
                    T* __restrict__ k_ret, T* __restrict__ v_ret) {
-  const int64_t head = blockIdx.x / n_blocks;
-  const int blk = (int)(blockIdx.x - head * n_blocks);
+  const int64_t head = (first + blockIdx.x) / (uint32_t)n_blocks;
+  const int blk = (int)(first + blockIdx.x - (uint32_t)head * (uint32_t)n_blocks);
   const int count = ret_count[head], left = (count < budget ? count : budget) - 32 * blk;
   if (left <= 0) return;
   const uint8_t* in = packed + (head * n_blocks + blk) * (int64_t)PackGeo<D>::kBlock;
@@ -202,7 +202,7 @@ bool kept_step_supported(const ltea_cfg& cfg, int n_seqs) {
   if (cfg.Hq / cfg.Hkv > kKeptMaxGroup) return false;
   // a head's scores are addressed by 32-bit offsets
   if (((int64_t)kept_blocks_of(cfg.window) + kept_blocks_of(cfg.budget)) * 128 * (cfg.Hq / cfg.Hkv) >= (int64_t)1 << 31) return false;
-  return (int64_t)n_seqs * cfg.Hkv <= ((int64_t)1 << 24);
+  return (int64_t)n_seqs * cfg.Hkv <= kMaxThreads / 256;      // (more heads than CUs: a workgroup of four waves each)
 }
 
 hipError_t launch_kept_step(const ltea_cfg& cfg, const void* q, const void* k, const void* v, void* out, const ltea_cache& c,
@@ -223,14 +223,19 @@ hipError_t launch_kept_convert(const ltea_cfg& cfg, const ltea_cache& c, void* p
   auto go = [&](auto tag, auto dim) {
     using T = decltype(tag);
     constexpr int D = decltype(dim)::value;
-    if (to_packed)
-      hipLaunchKernelGGL((kept_pack_kernel<T, D>), dim3((unsigned)grid), dim3(kPackThreads), 0, stream, static_cast<const T*>(c.k_ret),
-                         static_cast<const T*>(c.v_ret), c.ret_count, cfg.budget, n_blocks, static_cast<uint8_t*>(packed));
-    else
-      hipLaunchKernelGGL((kept_unpack_kernel<T, D>), dim3((unsigned)grid), dim3(kPackThreads), 0, stream,
-                         static_cast<const uint8_t*>(packed), c.ret_count, cfg.budget, n_blocks, static_cast<T*>(c.k_ret),
-                         static_cast<T*>(c.v_ret));
-    return hipGetLastError();
+    constexpr int64_t kMost = kMaxThreads / kPackThreads;
+    for (int64_t first = 0; first < grid; first += kMost) {
+      const dim3 blocks((unsigned)(grid - first < kMost ? grid - first : kMost));
+      if (to_packed)
+        hipLaunchKernelGGL((kept_pack_kernel<T, D>), blocks, dim3(kPackThreads), 0, stream, static_cast<const T*>(c.k_ret),
+                           static_cast<const T*>(c.v_ret), c.ret_count, cfg.budget, n_blocks, (uint32_t)first, static_cast<uint8_t*>(packed));
+      else
+        hipLaunchKernelGGL((kept_unpack_kernel<T, D>), blocks, dim3(kPackThreads), 0, stream, static_cast<const uint8_t*>(packed),
+                           c.ret_count, cfg.budget, n_blocks, (uint32_t)first, static_cast<T*>(c.k_ret), static_cast<T*>(c.v_ret));
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
   };
   if (cfg.dtype == LTEA_F32)
     return cfg.D == 64 ? go(float{}, std::integral_constant<int, 64>{}) : go(float{}, std::integral_constant<int, 128>{});

@@ -157,6 +157,9 @@ hipError_t launch_decode_step_lazy(const ltea_cfg& cfg, const void* q, const voi
                                    const ltea_cache& cache, int n_seqs, int32_t* status, void* workspace,
                                    hipStream_t stream);
 
+// A launch counts its threads in 32 bits: a grid of more runs without an error, and in part.
+constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;
+
 // ---- weights of a prompt, the step that evicts by them, kept rows in 4 bits (attention_mass.hip, kept.hip) --------------------
 size_t mass_workspace(const ltea_cfg& cfg, const SeqView& sv, int last);
 size_t mass_workspace_most(const ltea_cfg& cfg, int64_t total, int32_t max_seqlen);      // of any call of up to so many tokens
