@@ -380,7 +380,8 @@ int ltea_decode_step_mass(const ltea_cfg *cfg, const void *q, const void *k, con
 
 /* ltea_decode_step_lazy over a compact segment in 4 bits: keys are the scores that ltea_rescore writes, n_scored is
  * left alone, and a token that leaves the window without a final score is reported as there.  packed may be NULL where
- * budget is 0.  Workspace: ltea_decode_kept_workspace_bytes. */
+ * budget is 0.  LTEA_EUNSUPPORTED as above.  Its workspace holds no scores: less than a step by weight needs. */
+size_t ltea_decode_packed_workspace_bytes(const ltea_cfg *cfg, int32_t n_seqs);
 int ltea_decode_step_packed(const ltea_cfg *cfg, const void *q, const void *k, const void *v, void *out,
                             const ltea_cache *cache, void *packed, int32_t n_seqs, int32_t *status_or_null,
                             void *workspace, size_t workspace_bytes, void *stream);

@@ -66,7 +66,7 @@ EXPORTS = ["ltea_strerror", "ltea_cnn_panels_bytes", "ltea_cnn_prepare", "ltea_w
            "ltea_decode_step_feat", "ltea_cnn_backward_workspace_bytes", "ltea_cnn_backward", "ltea_lazy_period", "ltea_rescore_workspace_bytes", "ltea_rescore",
            "ltea_decode_step_lazy", "ltea_mass_workspace_bytes", "ltea_attention_mass", "ltea_prefill_mass_workspace_bytes",
            "ltea_prefill_mass", "ltea_packed_bytes", "ltea_kept_pack", "ltea_kept_unpack", "ltea_decode_kept_workspace_bytes",
-           "ltea_decode_step_mass", "ltea_decode_step_packed", "ltea_train_workspace_bytes", "ltea_train_forward", "ltea_train_backward",
+           "ltea_decode_step_mass", "ltea_decode_packed_workspace_bytes", "ltea_decode_step_packed", "ltea_train_workspace_bytes", "ltea_train_forward", "ltea_train_backward",
            "ltea_lambda_update", "ltea_diag_sink_bytes",
            "ltea_diag_mfma_loop", "ltea_diag_stream_read"]
 
@@ -156,6 +156,8 @@ def lib() -> C.CDLL:
     L.ltea_decode_kept_workspace_bytes.argtypes = [P(ltea_cfg), i32]
     L.ltea_decode_step_mass.restype = C.c_int
     L.ltea_decode_step_mass.argtypes = [P(ltea_cfg), vp, vp, vp, vp, P(ltea_cache), vp, i32, vp, sz, vp]
+    L.ltea_decode_packed_workspace_bytes.restype = sz
+    L.ltea_decode_packed_workspace_bytes.argtypes = [P(ltea_cfg), i32]
     L.ltea_decode_step_packed.restype = C.c_int
     L.ltea_decode_step_packed.argtypes = [P(ltea_cfg), vp, vp, vp, vp, P(ltea_cache), vp, i32, vp, vp, sz, vp]
     L.ltea_train_workspace_bytes.restype = sz
@@ -667,7 +669,11 @@ def ltea_decode_kept_workspace_bytes(cfg: ltea_cfg, n_seqs: int) -> int:
     return int(lib().ltea_decode_kept_workspace_bytes(C.byref(cfg), n_seqs))
 
 
-def _kept_step_tensors(cfg: ltea_cfg, q, k, v, cache, packed, out, workspace):
+def ltea_decode_packed_workspace_bytes(cfg: ltea_cfg, n_seqs: int) -> int:
+    return int(lib().ltea_decode_packed_workspace_bytes(C.byref(cfg), n_seqs))
+
+
+def _kept_step_tensors(cfg: ltea_cfg, q, k, v, cache, packed, out, workspace, workspace_bytes):
     B, D = q.shape[0], cfg.D
     td = torch.float32 if cfg.dtype == LTEA_F32 else torch.bfloat16
     device = _current_device(q, "q")
@@ -681,7 +687,7 @@ def _kept_step_tensors(cfg: ltea_cfg, q, k, v, cache, packed, out, workspace):
         out = torch.empty((B, cfg.Hq, D), dtype=td, device=q.device)
     else:
         _dense(out, (B, cfg.Hq, D), td, device, "out")
-    return B, out, _workspace_of(workspace, device, lambda: ltea_decode_kept_workspace_bytes(cfg, B))
+    return B, out, _workspace_of(workspace, device, lambda: workspace_bytes(cfg, B))
 
 
 def ltea_decode_step_mass(cfg: ltea_cfg, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: Cache,
@@ -689,7 +695,7 @@ def ltea_decode_step_mass(cfg: ltea_cfg, q: torch.Tensor, k: torch.Tensor, v: to
                           workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """A decode step that evicts by accumulated attention weight.  packed: the kept rows in 4 bits, in the place of cache.k_ret
     and cache.v_ret."""
-    B, out, workspace = _kept_step_tensors(cfg, q, k, v, cache, packed, out, workspace)
+    B, out, workspace = _kept_step_tensors(cfg, q, k, v, cache, packed, out, workspace, ltea_decode_kept_workspace_bytes)
     _check(lib().ltea_decode_step_mass(C.byref(cfg), _ptr(q), _ptr(k), _ptr(v), _ptr(out), C.byref(cache.struct), _ptr(packed), B,
                                        _ptr(workspace), workspace.numel(), _stream()), "ltea_decode_step_mass")
     return out
@@ -702,7 +708,7 @@ def ltea_decode_step_packed(cfg: ltea_cfg, q: torch.Tensor, k: torch.Tensor, v: 
     assert packed is not None, "packed: expected the kept rows in 4 bits"
     if status is not None:
         assert status.numel() >= 1 and status.dtype is torch.int32 and status.get_device() == q.get_device(), "status: expected an int32 on q's device"
-    B, out, workspace = _kept_step_tensors(cfg, q, k, v, cache, packed, out, workspace)
+    B, out, workspace = _kept_step_tensors(cfg, q, k, v, cache, packed, out, workspace, ltea_decode_packed_workspace_bytes)
     _check(lib().ltea_decode_step_packed(C.byref(cfg), _ptr(q), _ptr(k), _ptr(v), _ptr(out), C.byref(cache.struct), _ptr(packed), B,
                                          _ptr(status), _ptr(workspace), workspace.numel(), _stream()), "ltea_decode_step_packed")
     return out

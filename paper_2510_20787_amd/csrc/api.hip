@@ -662,7 +662,7 @@ int kept_step(const ltea_cfg* cfg, const void* q, const void* k, const void* v, 
   if (!q || !k || !v || !out) return LTEA_EINVAL;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return LTEA_EINVAL;
   if (!kept_step_supported(*cfg, n_seqs)) return LTEA_EUNSUPPORTED;
-  if (!workspace || workspace_bytes < align_up(kept_workspace(*cfg, n_seqs, packed != nullptr), 256)) return LTEA_EWORKSPACE;
+  if (!workspace || workspace_bytes < align_up(kept_workspace(*cfg, n_seqs, packed != nullptr, mass), 256)) return LTEA_EWORKSPACE;
   if (!aligned256(workspace)) return LTEA_EINVAL;
   return hip_status(launch_kept_step(*cfg, q, k, v, out, *cache, packed, mass, n_seqs, status, workspace,
                                      static_cast<hipStream_t>(stream)));
@@ -679,7 +679,12 @@ int ltea_kept_unpack(const ltea_cfg* cfg, const void* packed, const ltea_cache* 
 
 size_t ltea_decode_kept_workspace_bytes(const ltea_cfg* cfg, int32_t n_seqs) {
   if (check_cfg(cfg) != LTEA_OK || n_seqs < 0 || !kept_step_supported(*cfg, n_seqs)) return 0;
-  return align_up(kept_workspace_most(*cfg, n_seqs), 256);
+  return align_up(kept_workspace_most(*cfg, n_seqs, true), 256);
+}
+
+size_t ltea_decode_packed_workspace_bytes(const ltea_cfg* cfg, int32_t n_seqs) {
+  if (check_cfg(cfg) != LTEA_OK || n_seqs < 0 || !kept_step_supported(*cfg, n_seqs)) return 0;
+  return align_up(kept_workspace_most(*cfg, n_seqs, false), 256);
 }
 
 int ltea_decode_step_mass(const ltea_cfg* cfg, const void* q, const void* k, const void* v, void* out, const ltea_cache* cache,

@@ -19,7 +19,6 @@
 
 namespace ltea {
 
-constexpr int kPackRows = 32;
 template <int D> struct PackGeo {
   static constexpr int kBlock = 34 * D;                     // bytes of a block
   static constexpr int kV = 16 * D, kKe = 32 * D, kVe = 33 * D;   // offsets of its parts (K codes at 0)

@@ -177,10 +177,11 @@ KeptSplit split_of(const ltea_cfg& cfg, int n_seqs, bool packed) {
   return KeptSplit{(int)n, 4};
 }
 
-size_t kept_floats(const ltea_cfg& cfg, int64_t heads, int64_t shares) {
+// scored: heads whose scores are kept here.  (What shares hand over has its place also where heads are finished whole: a few KB a head.)
+size_t kept_floats(const ltea_cfg& cfg, int64_t heads, int64_t shares, int64_t scored) {
   const KeptLayout L{cfg.Hq / cfg.Hkv, cfg.D, 1, 32 * (kept_blocks_of(cfg.window) + kept_blocks_of(cfg.budget))};
   auto up = [](size_t x) { return (x + 63) / 64 * 64; };
-  return up(L.plan() * heads) + up(L.share() * shares) + L.scores() * heads;
+  return up(L.plan() * heads) + up(L.share() * shares) + L.scores() * scored;
 }
 
 }  // namespace
@@ -189,13 +190,18 @@ size_t kept_packed_bytes(const ltea_cfg& cfg, int n_seqs) {
   return (size_t)n_seqs * cfg.Hkv * kept_blocks_of(cfg.budget) * 34 * cfg.D;
 }
 
-size_t kept_workspace(const ltea_cfg& cfg, int n_seqs, bool packed) {
+size_t kept_workspace(const ltea_cfg& cfg, int n_seqs, bool packed, bool mass) {
   const int64_t heads = (int64_t)n_seqs * cfg.Hkv;
-  return heads == 0 ? 0 : kept_floats(cfg, heads, heads * split_of(cfg, n_seqs, packed).shares) * sizeof(float);
+  if (heads == 0) return 0;
+  const KeptSplit s = split_of(cfg, n_seqs, packed);
+  return kept_floats(cfg, heads, heads * s.shares, mass && !kept_form(cfg, s, mass).scores_in_lds ? heads : 0) * sizeof(float);
 }
-size_t kept_workspace_most(const ltea_cfg& cfg, int n_seqs) {      // with and without packed rows, and not less for more sequences
+// With and without packed rows, and not less for more sequences.  Scores: of all heads, or of no more than are ever cut or take eight waves.
+size_t kept_workspace_most(const ltea_cfg& cfg, int n_seqs, bool mass) {
   const int64_t heads = (int64_t)n_seqs * cfg.Hkv;
-  return heads == 0 ? 0 : kept_floats(cfg, heads, heads > kCus ? heads : kCus) * sizeof(float);
+  if (heads == 0) return 0;
+  const int64_t scored = heads > kCus && kept_form(cfg, KeptSplit{1, 4}, mass).scores_in_lds ? kCus : heads;
+  return kept_floats(cfg, heads, heads > kCus ? heads : kCus, mass ? scored : 0) * sizeof(float);
 }
 
 bool kept_step_supported(const ltea_cfg& cfg, int n_seqs) {

@@ -36,7 +36,7 @@ namespace {
 constexpr int kStepWaves = 4, kStepThreads = kStepWaves * kWave;     // of a workgroup that shares a head, and of the second launch
 
 struct KeptParams {
-  int B, Hq, Hkv, window, budget, sink, mass;
+  int Hq, Hkv, window, budget, sink, mass;
   int scores_in_lds;
   uint32_t count_mask;           // the bits of ret_count that are the count
   float tau, scale2;             // scale * log2(e)
@@ -1065,30 +1065,26 @@ hipError_t kept_run(const ltea_cfg& cfg, const KeptInputs& in, const ltea_cache&
                     hipStream_t stream) {
   CacheDev C{c.k_win, c.v_win, c.win_score, c.k_ret, c.v_ret, c.ret_score, c.ret_pos, c.ret_count, c.n_seen, c.n_scored};
   KeptParams P;
-  P.B = n_seqs; P.Hq = cfg.Hq; P.Hkv = cfg.Hkv; P.window = cfg.window; P.budget = cfg.budget; P.sink = cfg.sink;
+  P.Hq = cfg.Hq; P.Hkv = cfg.Hkv; P.window = cfg.window; P.budget = cfg.budget; P.sink = cfg.sink;
   P.mass = in.mass;
   P.tau = cfg.tau_logit;
   P.scale2 = (cfg.softmax_scale > 0.f ? cfg.softmax_scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
   P.packed = static_cast<const uint8_t*>(in.packed);
   P.status = in.status;
   const int G = cfg.Hq / cfg.Hkv, nsplit = split.shares;
+  const KeptForm form = kept_form(cfg, split, in.mass);
   P.L = KeptLayout{G, D, nsplit, 32 * (kept_blocks_of(cfg.window) + kept_blocks_of(cfg.budget))};
-  // a whole head's workgroup finishes it where its count fits ret_count's upper bits
-  const bool whole = nsplit == 1 && cfg.budget > 0 && cfg.budget < (1 << 16) && cfg.Hkv <= 255;
-  P.count_mask = whole ? 0xFFFFu : 0xFFFFFFFFu;
+  P.count_mask = form.whole ? 0xFFFFu : 0xFFFFFFFFu;
+  P.scores_in_lds = form.scores_in_lds;
   const int64_t heads = (int64_t)n_seqs * cfg.Hkv;
   P.plan = static_cast<float*>(workspace);
   P.shares = P.plan + (P.L.plan() * heads + 63) / 64 * 64;
-  P.scores = P.shares + (P.L.share() * heads * nsplit + 63) / 64 * 64;
+  P.scores = P.shares + (P.L.share() * heads * nsplit + 63) / 64 * 64;      // (there by weight only, where they are not in LDS)
   const dim3 grid((unsigned)(heads * nsplit));
   auto launch = [&](auto pk, auto gt, auto finishes, auto waves) {
     constexpr bool PK = decltype(pk)::value, WHOLE = decltype(finishes)::value;
     constexpr int GT = decltype(gt)::value, W = decltype(waves)::value;
-    size_t bytes = ((size_t)W * (G < GT ? G : GT) * (D + 4) + 6 * (size_t)G + 4) * sizeof(float);
-    const size_t rest = in.mass ? P.L.scores() * sizeof(float) : 0;
-    P.scores_in_lds = WHOLE && rest <= kKeptScoresLds && bytes + rest <= kKeptLds;
-    if (P.scores_in_lds) bytes += rest;
-    hipLaunchKernelGGL((kept_step_kernel<T, D, PK, GT, WHOLE, W>), grid, dim3(W * kWave), bytes, stream, C, P,
+    hipLaunchKernelGGL((kept_step_kernel<T, D, PK, GT, WHOLE, W>), grid, dim3(W * kWave), form.lds, stream, C, P,
                        static_cast<const T*>(in.q), static_cast<const T*>(in.k), static_cast<const T*>(in.v), static_cast<T*>(in.out));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || WHOLE) return e;
@@ -1100,9 +1096,8 @@ hipError_t kept_run(const ltea_cfg& cfg, const KeptInputs& in, const ltea_cache&
   using std::true_type;
   auto go = [&](auto pk, auto gt) {
     const integral_constant<int, kStepWaves> four;
-    if (!whole) return launch(pk, gt, std::false_type{}, four);
-    // (the outputs of eight waves: 34 KB of LDS)
-    if (split.waves == 8 && (G < decltype(gt)::value ? G : decltype(gt)::value) * D <= 1024) return launch(pk, gt, true_type{}, integral_constant<int, 8>{});
+    if (!form.whole) return launch(pk, gt, std::false_type{}, four);
+    if (form.waves == 8) return launch(pk, gt, true_type{}, integral_constant<int, 8>{});
     return launch(pk, gt, true_type{}, four);
   };
   auto by_heads = [&](auto pk) {

@@ -168,8 +168,8 @@ hipError_t launch_attention_mass(const ltea_cfg& cfg, const void* q, int64_t q_s
                                  int64_t k_stride_tok, int64_t k_stride_head, const SeqView& sv, const float* lse, int last,
                                  float* mass, void* workspace, hipStream_t stream);
 size_t kept_packed_bytes(const ltea_cfg& cfg, int n_seqs);
-size_t kept_workspace(const ltea_cfg& cfg, int n_seqs, bool packed);
-size_t kept_workspace_most(const ltea_cfg& cfg, int n_seqs);                            // of any step of up to so many sequences
+size_t kept_workspace(const ltea_cfg& cfg, int n_seqs, bool packed, bool mass);
+size_t kept_workspace_most(const ltea_cfg& cfg, int n_seqs, bool mass);                 // of any step of up to so many sequences
 bool kept_step_supported(const ltea_cfg& cfg, int n_seqs);
 // packed (or null): the kept rows in 4 bits, in the place of c.k_ret, c.v_ret.  mass: evicts by accumulated weight, else by the
 // keys as they are.
