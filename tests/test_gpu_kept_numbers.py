@@ -149,3 +149,38 @@ def test_probabilities_keep_32_bits(D, G, segment):
     assert (np.abs(ref[own]) <= 2.0 ** -14 * terms[own]).all()
     err = np.abs(got - ref)
     assert (err <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -20 * terms)[own].all(), float((err / terms)[own].max() * 2 ** 20)
+
+
+def check_added(got, before, after, where):
+    """Keys against what they were and what 64 bits add: half a step of fp32 of the sum and 2^-15 of the weight that is added, whatever the
+    key.  (A weight: 2^-18 of each of its probabilities, as in check(), their sum's and their normaliser's roundings; the numbers of some
+    ten below 2^-126 that a probability in fp32 cannot be count as nothing.)"""
+    fine = np.isfinite(after)
+    assert np.array_equal(np.isinf(got), np.isinf(after)), where
+    added = after[fine] - before[fine]
+    err = np.abs(got[fine] - after[fine])
+    assert (err <= 2.0 ** -24 * after[fine] + 2.0 ** -15 * added + 2.0 ** -120).all(), (where, float((err / after[fine]).max()))
+    return float(np.median(added))
+
+
+@pytest.mark.parametrize("packed", [False, True], ids=["rows", "packed"])
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("small_keys", [False, True], ids=["keys", "small keys"])
+@pytest.mark.parametrize("nb,G,window,budget,every", [(2, 2, 60, 5000, 1), (1, 8, 300, 3000, 1), (150, 4, 45, 70, 41), (60, 9, 70, 100, 17)])
+def test_added_weights(nb, G, window, budget, every, small_keys, dtype, D, packed):
+    """What a step adds to the keys of ring and kept entries, also where it is a small part of them."""
+    cfg = B.make_cfg(2 * G, 2, D, window, budget, 1, 0.0, 0.0, dtype)
+    cache = make_state(cfg, [window + budget + 5 + i for i in range(nb)], [budget] * nb, 45)
+    if small_keys:
+        cache.win_score.mul_(2.0 ** -20), cache.ret_score.mul_(2.0 ** -20)
+    pk = B.ltea_kept_pack(cfg, cache) if packed else None
+    before = clone(cache)
+    medians = []
+    for b, h, _, _, _, st in one_step(cfg, cache, pk, True, 46, every):
+        slot, win, ret = int(before.n_seen[b]) % window, f64(before.win_score[b, h]), f64(before.ret_score[b, h])
+        if st["dst"] is not None:
+            ret[st["dst"]] = win[slot]
+        win[slot] = 0.0
+        medians += [check_added(f64(cache.win_score[b, h]), win, st["win_key"], (b, h)),
+                    check_added(f64(cache.ret_score[b, h]), ret, st["ret_key"], (b, h))]
+    assert 0 < min(medians) and max(medians) < 0.2
