@@ -329,8 +329,9 @@ int ltea_decode_step_lazy(const ltea_cfg *cfg, const void *q, const void *k, con
  *
  * ltea_attention_mass: mass[h][j] = sum over the query heads hq of KV head h and the queries i of j's sequence with
  * j <= i < j + window and i >= n - last (last <= 0: all queries) of exp(scale * q_i . k_j - lse[hq][i]).
- * lse: [Hq][total_tokens] fp32, the natural log of query i's softmax normaliser (ltea_train_forward writes it); a query
- * whose lse is not finite counts nothing.  mass: [Hkv][total_tokens] fp32.  q, k: views as in ltea_prefill.  Of the
+ * lse: [Hq][total_tokens] fp32, the natural log of query i's softmax normaliser (ltea_train_forward writes it: on bf16 storage
+ * that of probabilities rounded to bf16, which shows in a weight by up to 2^-8 of it; ltea_prefill_mass takes it in 32 bits); a
+ * query whose lse is not finite counts nothing.  mass: [Hkv][total_tokens] fp32.  q, k: views as in ltea_prefill.  Of the
  * config budget, sink and tau_logit are ignored.  Same bits every time.  LTEA_EUNSUPPORTED: query rows of 2^24 bytes and more apart, or
  * (total_tokens / 256 + n_seqs) * (Hkv + 7) of 2^24 and more (fp32: total_tokens / 128). */
 size_t ltea_mass_workspace_bytes(const ltea_cfg *cfg, int32_t n_seqs, int64_t total_tokens, int32_t max_seqlen);

@@ -112,9 +112,9 @@ int do_score(const ltea_cfg& cfg, const ltea_cnn& cnn, const void* k, const void
 
 int do_attention(const ltea_cfg& cfg, const void* q, int64_t qst, int64_t qsh, const void* k, const void* v,
                  int64_t st, int64_t sh, const SeqView& sv, const ltea_cache& c, void* out, hipStream_t stream,
-                 float* lse = nullptr) {
+                 float* lse = nullptr, bool full = false) {
   if (attention_mfma_supported(cfg, st, sv.max_seqlen))
-    return hip_status(launch_attention_mfma(cfg, q, qst, qsh, k, v, st, sh, sv, c, out, stream, nullptr, nullptr, lse));
+    return hip_status(launch_attention_mfma(cfg, q, qst, qsh, k, v, st, sh, sv, c, out, stream, nullptr, nullptr, lse, full));
   return hip_status(launch_attention_generic(cfg, q, qst, qsh, k, v, st, sh, sv, c, out, stream, lse));
 }
 
@@ -626,7 +626,7 @@ int ltea_prefill_mass(const ltea_cfg* cfg, const void* q, int64_t q_stride_tok, 
   float* mass = mass_or_null ? mass_or_null : reinterpret_cast<float*>(ws + lse_bytes);
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (total_tokens > 0) {
-    st = do_attention(open, q, q_stride_tok, q_stride_head, k, v, kv_stride_tok, kv_stride_head, sv, *cache, out, s, lse);
+    st = do_attention(open, q, q_stride_tok, q_stride_head, k, v, kv_stride_tok, kv_stride_head, sv, *cache, out, s, lse, true);
     if (st != LTEA_OK) return st;
     st = hip_status(launch_attention_mass(open, q, q_stride_tok, q_stride_head, k, kv_stride_tok, kv_stride_head, sv, lse, last, mass,
                                           ws + lse_bytes + mass_bytes, s));

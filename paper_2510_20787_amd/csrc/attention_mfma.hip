@@ -84,7 +84,9 @@ template <int D> __device__ __forceinline__ int piece_swizzle(int row) { return 
 // sees the same window, so a block is plain, masked or out of reach for all four at once (with HW = 1 the waves' windows
 // are shifted by 32 positions each, the workgroup's key range is 96 positions longer, and waves wait for each other at
 // the tile barrier).
-template <int D, int HW>
+// FULL: lse is that of the probabilities before they are rounded for the product.  The output is divided by the sum of what it is made of
+// either way; a normaliser that others are divided by is not (off by up to 2^-9 of itself by the rounding).
+template <int D, int HW, bool FULL>
 __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2)
 attention_mfma_kernel(const bf16_t* __restrict__ q, int64_t q_st, int64_t q_sh, const bf16_t* __restrict__ k,
                       const bf16_t* __restrict__ v, int64_t kv_st, int64_t kv_sh, const int32_t* __restrict__ cu,
@@ -240,7 +242,7 @@ attention_mfma_kernel(const bf16_t* __restrict__ q, int64_t q_st, int64_t q_sh, 
   };
 
   // ---- softmax state (per lane = per query; the two lane halves keep separate partial sums) ------
-  float m_run, l_part;
+  float m_run, l_part, l_full;
   // Row sums of the tiles that are interleaved, on the matrix pipe: v_mfma_f32_16x16x32_bf16 reads a P operand of the value product
   // as 16 columns of which lane groups 0, 2 hold queries 0..15 and groups 1, 3 queries 16..31.  With ones in the rows whose
   // lowest bit is the group's, register 0 of every lane is the sum of query lane%16 and register 1 that of query
@@ -261,7 +263,7 @@ attention_mfma_kernel(const bf16_t* __restrict__ q, int64_t q_st, int64_t q_sh, 
     all_have_m = false;
     raised = 0;
     m_run = -INFINITY;
-    l_part = 0.f;
+    l_part = l_full = 0.f;
     l_mat = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int db = 0; db < ND; ++db)
@@ -314,6 +316,7 @@ attention_mfma_kernel(const bf16_t* __restrict__ q, int64_t q_st, int64_t q_sh, 
     const bool none = m_run == -INFINITY;
     m_run = m_new;
     l_part *= a;
+    if constexpr (FULL) l_full *= a;
     // A row that has seen nothing has nothing to scale: the first block waits for no accumulator.  (Short windows feel it: 4 x 4096
     // tokens, 16 heads of D = 128, window 16 55.6 -> 54.4 us.)
     if (__builtin_amdgcn_ballot_w64(a != 1.0f && !none) != 0ull) {
@@ -332,13 +335,16 @@ attention_mfma_kernel(const bf16_t* __restrict__ q, int64_t q_st, int64_t q_sh, 
   // scores and of block 0's value product is followed by its share of the other block's exponentials.
   auto tile_interleaved = [&](auto par, auto MASKED, int t) __attribute__((always_inline)) {
     constexpr int EPM = 16 / NK, HALF = NK / 2;     // operands are read HALF instructions ahead: further ahead spills
-    float e[16];
+    float e[16], block_sum = 0.f;
     auto exp_part = [&](int i, const f32x16& x) __attribute__((always_inline)) {
 #pragma unroll
       for (int r = EPM * i; r < EPM * (i + 1); ++r) {
         e[r] = __builtin_amdgcn_exp2f(fmaf(x[r], scale_log2e, -m_run));
         asm volatile("" : "+v"(e[r]));      // here, not next to its first use
+        if constexpr (FULL) block_sum = r == 0 ? e[r] : block_sum + e[r];
       }
+      if constexpr (FULL)
+        if (i == NK - 1) l_full += block_sum;
     };
     auto pack_part = [&](int i, bf16x8 (&p)[2]) __attribute__((always_inline)) {      // of the step before
 #pragma unroll
@@ -412,8 +418,14 @@ attention_mfma_kernel(const bf16_t* __restrict__ q, int64_t q_st, int64_t q_sh, 
     apply_mask(i, x);
     if (!all_have_m || exact_pass) raise_reference(x);
     const float m_use = (m_run == -INFINITY) ? 0.f : m_run;
+    float full = 0.f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) p[r / 8][r % 8] = static_cast<bf16_t>(__builtin_amdgcn_exp2f(fmaf(x[r], scale_log2e, -m_use)));
+    for (int r = 0; r < 16; ++r) {
+      const float e = __builtin_amdgcn_exp2f(fmaf(x[r], scale_log2e, -m_use));
+      p[r / 8][r % 8] = static_cast<bf16_t>(e);
+      if constexpr (FULL) full += e;
+    }
+    if constexpr (FULL) l_full += full;
     pin(p[0]);
     pin(p[1]);
     // row sum from the rounded probabilities: the denominator then matches the P that the product consumes
@@ -520,10 +532,11 @@ attention_mfma_kernel(const bf16_t* __restrict__ q, int64_t q_st, int64_t q_sh, 
   __syncthreads();  // tile buffers are free
   const float l_row = pair_sum(l_part) + ((lane & 16) != 0 ? l_mat[1] : l_mat[0]);
   const float inv = 1.0f / l_row;
+  const float l_all = FULL ? pair_sum(l_full) : 0.f;
   if (lse != nullptr && hb == 0) {
     // natural-log normaliser of the scaled scores (m_run is kept in the base-2 domain); wanted by a backward pass
     const int row = (HW == 1 ? 32 * wv : 0) + ql;
-    if (i0 + row < n) lse[(int64_t)hq * lse_stride + lo_q + i0 + row - q_begin] = (m_run + __log2f(l_row)) * 0.6931471805599453f;
+    if (i0 + row < n) lse[(int64_t)hq * lse_stride + lo_q + i0 + row - q_begin] = (m_run + __log2f(FULL ? l_all : l_row)) * 0.6931471805599453f;
   }
   bf16_t* orow = lds + (32 * wv + ql) * G::OS + 4 * hb;
 #pragma unroll
@@ -553,7 +566,7 @@ attention_mfma_kernel(const bf16_t* __restrict__ q, int64_t q_st, int64_t q_sh, 
   }
 }
 
-template <int D, int HW>
+template <int D, int HW, bool FULL>
 hipError_t run(const ltea_cfg& cfg, const void* q, int64_t q_st, int64_t q_sh, const void* k, const void* v,
                int64_t kv_st, int64_t kv_sh, const SeqView& sv, const ltea_cache& c, void* out,
                const int32_t* kv_start, const int32_t* kv_len, float* lse, hipStream_t stream) {
@@ -562,7 +575,7 @@ hipError_t run(const ltea_cfg& cfg, const void* q, int64_t q_st, int64_t q_sh, c
   const int64_t tiles_upper = (sv.total_tokens + BMQ - 1) / BMQ + sv.n_seqs;
   const int64_t n_work = tiles_upper * (cfg.Hq / HW);
   const int64_t grid = (n_work + 7) / 8 * 8;
-  hipLaunchKernelGGL((attention_mfma_kernel<D, HW>), dim3((unsigned)grid), dim3(kThreads), 0, stream,
+  hipLaunchKernelGGL((attention_mfma_kernel<D, HW, FULL>), dim3((unsigned)grid), dim3(kThreads), 0, stream,
                      static_cast<const bf16_t*>(q), q_st, q_sh, static_cast<const bf16_t*>(k),
                      static_cast<const bf16_t*>(v), kv_st, kv_sh, sv.cu_seqlens, sv.n_seqs, (int)tiles_upper,
                      (int)n_work, cfg.Hq, cfg.Hkv, cfg.window, cfg.budget, scale * 1.4426950408889634f,
@@ -582,15 +595,18 @@ bool attention_mfma_supported(const ltea_cfg& cfg, int64_t kv_stride_tok, int32_
 hipError_t launch_attention_mfma(const ltea_cfg& cfg, const void* q, int64_t q_st, int64_t q_sh, const void* k,
                                  const void* v, int64_t kv_st, int64_t kv_sh, const SeqView& sv, const ltea_cache& c,
                                  void* out, hipStream_t stream, const int32_t* kv_start, const int32_t* kv_len,
-                                 float* lse) {
+                                 float* lse, bool full) {
   if (sv.total_tokens == 0) return hipSuccess;
   // grouped-query shapes with a multiple of four query heads per KV head: one query head per wave (see the kernel)
   const bool by_head = (cfg.Hq / cfg.Hkv) % 4 == 0;
-  if (cfg.D == 64)
-    return by_head ? run<64, 4>(cfg, q, q_st, q_sh, k, v, kv_st, kv_sh, sv, c, out, kv_start, kv_len, lse, stream)
-                   : run<64, 1>(cfg, q, q_st, q_sh, k, v, kv_st, kv_sh, sv, c, out, kv_start, kv_len, lse, stream);
-  return by_head ? run<128, 4>(cfg, q, q_st, q_sh, k, v, kv_st, kv_sh, sv, c, out, kv_start, kv_len, lse, stream)
-                 : run<128, 1>(cfg, q, q_st, q_sh, k, v, kv_st, kv_sh, sv, c, out, kv_start, kv_len, lse, stream);
+  auto go = [&](auto dim, auto heads) {
+    constexpr int D = decltype(dim)::value, HW = decltype(heads)::value;
+    return full ? run<D, HW, true>(cfg, q, q_st, q_sh, k, v, kv_st, kv_sh, sv, c, out, kv_start, kv_len, lse, stream)
+                : run<D, HW, false>(cfg, q, q_st, q_sh, k, v, kv_st, kv_sh, sv, c, out, kv_start, kv_len, lse, stream);
+  };
+  using std::integral_constant;
+  if (cfg.D == 64) return by_head ? go(integral_constant<int, 64>{}, integral_constant<int, 4>{}) : go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  return by_head ? go(integral_constant<int, 128>{}, integral_constant<int, 4>{}) : go(integral_constant<int, 128>{}, integral_constant<int, 1>{});
 }
 
 }  // namespace ltea

@@ -101,8 +101,9 @@ hipError_t launch_attention_mfma(const ltea_cfg& cfg, const void* q, int64_t q_s
                                  const void* k, const void* v, int64_t kv_stride_tok, int64_t kv_stride_head,
                                  const SeqView& sv, const ltea_cache& cache, void* out, hipStream_t stream,
                                  const int32_t* kv_start = nullptr, const int32_t* kv_len = nullptr,
-                                 float* lse = nullptr);
-// lse (optional, both launchers): [Hq][total_tokens] fp32, natural log of each query's softmax normaliser.
+                                 float* lse = nullptr, bool full = false);
+// lse (optional, both launchers): [Hq][total_tokens] fp32, natural log of each query's softmax normaliser: the sum that its output was
+// divided by, which on the matrix cores is that of probabilities rounded to bf16, or (full) of the probabilities themselves.
 
 // ---- continuation of a prefill onto an existing cache ---------------------------------------------------
 // Device buffers of the "extended sequences" (pad | old kept entries by position | ring tokens | new tokens) that
