@@ -342,7 +342,8 @@ int ltea_attention_mass(const ltea_cfg *cfg, const void *q, int64_t q_stride_tok
 
 /* Prefill of such a cache: every query of a prompt sees everything before it (cfg->window does not limit the prompt),
  * mass is taken over the last `last` queries of each sequence (<= 0: all), and ltea_retain on it with rho = 0 fills the
- * cache.  Arguments as ltea_prefill; mass_or_null, if given, receives the [Hkv][total_tokens] weights. */
+ * cache.  Arguments as ltea_prefill; mass_or_null, if given, receives the [Hkv][total_tokens] weights.  What it leaves is for
+ * ltea_decode_step_mass: ltea_prefill_append continues caches whose keys are logits. */
 size_t ltea_prefill_mass_workspace_bytes(const ltea_cfg *cfg, int32_t n_seqs, int64_t total_tokens, int32_t max_seqlen);
 int ltea_prefill_mass(const ltea_cfg *cfg, const void *q, int64_t q_stride_tok, int64_t q_stride_head, const void *k,
                       const void *v, int64_t kv_stride_tok, int64_t kv_stride_head, const int32_t *cu_seqlens,
@@ -362,7 +363,7 @@ int ltea_prefill_mass(const ltea_cfg *cfg, const void *q, int64_t q_stride_tok, 
  *   D =  64: K codes [d/16][a][b][j][8 bytes]    V codes [a][d/4][j][b][2 bytes]
  *   K exponents [a][b][d/32][j]    V exponents [a][d/32][j][b]
  * ltea_kept_pack writes the rows of the first ret_count slots of every head from k_ret, v_ret; ltea_kept_unpack writes k_ret, v_ret
- * from them (to continue a prefill, say).  Other slots and members are not touched: a packed cache shares win_*, ret_score, ret_pos
+ * from them (to continue a cache that evicts by scores with another chunk of prompt, say).  Other slots and members are not touched: a packed cache shares win_*, ret_score, ret_pos
  * and the counters with the cache that it was packed from. */
 size_t ltea_packed_bytes(const ltea_cfg *cfg, int32_t n_seqs);
 int ltea_kept_pack(const ltea_cfg *cfg, const ltea_cache *cache, void *packed, int32_t n_seqs, void *stream);

@@ -155,7 +155,8 @@ kept_unpack_kernel(const uint8_t* __restrict__ packed, const int32_t* __restrict
 
 // Workgroups (shares) of a head and their waves.  A launch takes 256 CUs.
 // More heads than CUs: a head's workgroup of four waves, several of them on a CU (1024 heads of 1024 + 512 rows, D = 128: 136 us, with
-// eight waves 156; 512 heads of packed rows 86 and 99).  Fewer: eight waves (256 heads of 512 + 8192 packed rows, D = 128: 73 us, with
+// eight waves 156; 257, 300 and 384 heads of them 54, 56 and 59 us, with eight 64, 66 and 68; 257, 384 and 512 heads of 1024 + 2400 packed rows
+// 68, 74 and 84, with eight 79, 88 and 100; of 768 + 512 rows with four query heads, D = 64, 27.7, 30.4 and 32.5, with eight 28.1, 30.9 and 32.8).  Fewer: eight waves (256 heads of 512 + 8192 packed rows, D = 128: 73 us, with
 // four 85), but four for few short heads (8 heads of 768 + 512 rows 15.4 us, with eight 16.3; 64 heads 17.5 and 17.8).
 // Few heads of 48 blocks of rows or more are cut, in 8 shares or a power of two that leaves each 16 blocks: 8 heads of 768 + 1024 rows 16.1
 // us in 8 (whole 18.2, in 5 17.0), 32 of 768 + 2001 packed 15.7 in 8 (whole 20.6, in 6 and 10 16.5 and 17.4), 8 of 768 + 16384 packed 21.3
