@@ -7,11 +7,12 @@
 // A lane owns one query column, so lse is one register, and keeps sums of its 16 keys per block that meet over the lanes once, at
 // the end.  Products of bf16 values are exact in fp32 and nothing is rounded to fewer bits.
 //
-// Bound: a wave's issue.  32 x 32 scores take 128 cycles of exponentials and 128 of scale and sum beside 64 (D = 64) or 128 (D = 128)
-// of matrix instructions, which overlap little: 4 x 4096 tokens, 32/8 heads, D = 64: 223 us (615 TFLOP/s of products; vector instructions
-// issue in 77 % of the clocks in which a CU has work, matrix instructions in 31 %, and it has some in 79 %: 2176 workgroups in 768 places),
-// 32768 tokens, 32 heads, D = 128: 4270 us (1.03 PFLOP/s; 4190 to 4460 over several boxes; 67 %, 51 % and 96 %).  Two blocks of 32 keys per wave: at D = 64 three take 271 us and four 342 (fewer waves);
-// 16 x 16 instructions 8515 us for the long prompt where these took 4560 at the time (registers).
+// Bound: a wave's issue.  32 x 32 scores take 128 cycles of exponentials and 128 of scale and sum beside 64 (D = 64) or 128 (D =
+// 128) of matrix instructions, which overlap little: 4 x 4096 tokens, 32/8 heads, D = 64: 223 us (615 TFLOP/s of products; vector
+// instructions issue in 77 % of the clocks in which a CU has work, matrix instructions in 31 %, and it has some in 79 %: 2176
+// workgroups in 768 places), 32768 tokens, 32 heads, D = 128: 4270 us (1.03 PFLOP/s; 4190 to 4460 over several boxes; 67 %, 51 %
+// and 96 %).  Two blocks of 32 keys per wave: at D = 64 three take 271 us and four 342 (fewer waves); 16 x 16 instructions 8515 us
+// for the long prompt where these took 4560 at the time (registers).
 //
 // A workgroup takes 4 waves x KB blocks of 32 keys of one (sequence, KV head) and a part of the queries that can see them, all
 // query heads of the group.  Parts meet in a second launch, in their order: same bits every time, and sums of at most 2048 queries

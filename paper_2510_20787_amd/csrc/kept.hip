@@ -154,16 +154,18 @@ kept_unpack_kernel(const uint8_t* __restrict__ packed, const int32_t* __restrict
 }
 
 // Workgroups (shares) of a head and their waves.  A launch takes 256 CUs.
-// More heads than CUs: a head's workgroup of four waves, several of them on a CU (1024 heads of 1024 + 512 rows, D = 128: 136 us, with
-// eight waves 156; 257, 300 and 384 heads of them 54, 56 and 59 us, with eight 64, 66 and 68; 257, 384 and 512 heads of 1024 + 2400 packed rows
-// 68, 74 and 84, with eight 79, 88 and 100; of 768 + 512 rows with four query heads, D = 64, 27.7, 30.4 and 32.5, with eight 28.1, 30.9 and 32.8).  Fewer: eight waves (256 heads of 512 + 8192 packed rows, D = 128: 73 us, with
-// four 85), but four for few short heads (8 heads of 768 + 512 rows 15.4 us, with eight 16.3; 64 heads 17.5 and 17.8).
-// Few heads of 48 blocks of rows or more are cut, in 8 shares or a power of two that leaves each 16 blocks: 8 heads of 768 + 1024 rows 16.1
-// us in 8 (whole 18.2, in 5 17.0), 32 of 768 + 2001 packed 15.7 in 8 (whole 20.6, in 6 and 10 16.5 and 17.4), 8 of 768 + 16384 packed 21.3
-// in 16 and 21.0 in 32 (whole 73.9, in 8 26.5), 8 of 768 + 32768 packed 23.4 in 32 (in 16 and 64 27.2 and 30.4: reading the shares grows
-// with them); wide rows in more, a share for each 128 KB (2 heads of 768 + 4000 fp32 rows, D = 128: 22.7 us in 32, 25.9 in 16, 25.0 in 64;
-// 4 of 768 + 16384: 33.4 in 64, 37.7 in 32).  Shorter heads do not gain (40 blocks: 15.4 us whole and in 8).  Where a head gets fewer than four CUs packed rows do
-// not gain either (128 heads of 1024 + 8192: 45 us whole, 47 in 2), stored ones do (128 of 1024 + 2048: 55 whole, 43 in 2).
+// More heads than CUs: a head's workgroup of four waves, several of them on a CU (1024 heads of 1024 + 512 rows, D = 128: 136 us,
+// with eight waves 156; 257, 300 and 384 heads of them 54, 56 and 59 us, with eight 64, 66 and 68; 257, 384 and 512 heads of 1024 +
+// 2400 packed rows 68, 74 and 84, with eight 79, 88 and 100; of 768 + 512 rows with four query heads, D = 64, 27.7, 30.4 and 32.5,
+// with eight 28.1, 30.9 and 32.8).  Fewer: eight waves (256 heads of 512 + 8192 packed rows, D = 128: 73 us, with four 85), but
+// four for few short heads (8 heads of 768 + 512 rows 15.4 us, with eight 16.3; 64 heads 17.5 and 17.8). Few heads of 48 blocks of
+// rows or more are cut, in 8 shares or a power of two that leaves each 16 blocks: 8 heads of 768 + 1024 rows 16.1 us in 8 (whole
+// 18.2, in 5 17.0), 32 of 768 + 2001 packed 15.7 in 8 (whole 20.6, in 6 and 10 16.5 and 17.4), 8 of 768 + 16384 packed 21.3 in 16
+// and 21.0 in 32 (whole 73.9, in 8 26.5), 8 of 768 + 32768 packed 23.4 in 32 (in 16 and 64 27.2 and 30.4: reading the shares grows
+// with them); wide rows in more, a share for each 128 KB (2 heads of 768 + 4000 fp32 rows, D = 128: 22.7 us in 32, 25.9 in 16, 25.0
+// in 64; 4 of 768 + 16384: 33.4 in 64, 37.7 in 32).  Shorter heads do not gain (40 blocks: 15.4 us whole and in 8).  Where a head
+// gets fewer than four CUs packed rows do not gain either (128 heads of 1024 + 8192: 45 us whole, 47 in 2), stored ones do (128 of
+// 1024 + 2048: 55 whole, 43 in 2).
 constexpr int64_t kCus = 256;
 KeptSplit split_of(const ltea_cfg& cfg, int n_seqs, bool packed) {
   const int64_t heads = (int64_t)n_seqs * cfg.Hkv, G = cfg.Hq / cfg.Hkv, fill = kCus / heads;
